@@ -83,7 +83,8 @@ typedef enum {
   BIFATTN_EHIP = -5,         /* a HIP runtime call or kernel launch failed */
   BIFATTN_ELENS = -6,        /* a decode length was outside [0, m_d_max] */
   BIFATTN_ESCALE = -7,       /* a key or value scale was not a positive normal float */
-  BIFATTN_ESCRATCH = -8      /* bifattn_decode_noalloc: workspace beyond its fixed scratch */
+  BIFATTN_ESCRATCH = -8,     /* bifattn_decode_noalloc: workspace beyond its fixed scratch */
+  BIFATTN_EPAGE = -9         /* paged caches: a page id was outside the pool */
 } bifattn_status_t;
 
 /* Which computation bifattn_decode runs (bifattn_dims_t.path). The FAQ on
@@ -102,8 +103,11 @@ typedef enum {
   BIFATTN_KV_BF16 = 0,     /* bf16 keys and values */
   BIFATTN_KV_FP8_E4M3 = 1, /* OCP 8-bit float E4M3 codes (bias 7, no infinities, max 448) */
   BIFATTN_KV_INT8 = 2,     /* two's complement 8-bit integer codes */
-  BIFATTN_KV_INT4 = 3      /* two's complement 4-bit integer codes, two per byte: element u
+  BIFATTN_KV_INT4 = 3,     /* two's complement 4-bit integer codes, two per byte: element u
                               of a row in byte u/2, even u in the low nibble; rows d/2 bytes */
+  BIFATTN_KV_MXFP4 = 4     /* paged caches only: OCP MXFP4, 4-bit floats E2M1 (0, 0.5, 1, 1.5,
+                              2, 3, 4, 6 and their negatives), two per byte like INT4, and one
+                              scale byte e per 32 elements, 2^(e - 127), 255 = NaN */
 } bifattn_kv_type_t;
 
 /* Problem dimensions (Section 3.1 notation; d is the head dimension). */
@@ -332,6 +336,148 @@ bifattn_status_t bifattn_decode_noalloc(const bifattn_dims_t *dims, const void *
                                         const void *Vc, const void *Kd, const void *Vd,
                                         const int32_t *decode_lens, const float *k_scale,
                                         const float *v_scale, float *out, hipStream_t stream);
+
+/*
+ * Paged caches. All rows lie in one pool of pages that the caller owns; a
+ * table of page ids (int32) names the pages of a sequence in order, so row t of
+ * a sequence is row t % page of page table[t / page]. The context is one
+ * sequence of m_c rows that all samples share; every sample owns a sequence
+ * of up to m_d_max rows, its decode rows. The two never share a page that is
+ * written. Table entries past a sequence's last valid row are never used and
+ * may hold anything, and so may the rows of a page past it.
+ *
+ *   K, V          kv [num_pages][g][page][d]   (8-bit codes one byte, MXFP4 two codes a byte)
+ *   K_exp, V_exp  uint8 [num_pages][g][page][d/32]  scale bytes, MXFP4 only, else NULL
+ *   k_scale, v_scale fp32 [g] (device), fp8 only, or NULL for 1; as in bifattn_decode_scaled
+ *
+ * An id outside [0, num_pages) is not followed: attention reads page 0 in its
+ * place, append and read-out skip its rows, and all raise a sticky flag that
+ * bifattn_paged_plan_status reports as BIFATTN_EPAGE.
+ */
+typedef struct {
+  void *K, *V;
+  uint8_t *K_exp, *V_exp;
+  const float *k_scale, *v_scale;
+} bifattn_pages_t;
+
+/* Dimensions of a paged plan; those of bifattn_dims_t unless said otherwise. */
+typedef struct {
+  int32_t b, h, g;
+  int32_t d;         /* elements of a row: 64 or 128 */
+  int32_t m_c;       /* shared context rows, >= 0 */
+  int32_t m_d_max;   /* row capacity of every sample, >= 0; m_c + m_d_max >= 1 */
+  int32_t page;      /* rows of a page: 16, 32, 64, 128 or 256 */
+  int32_t num_pages; /* pages of the pool, >= 1 */
+  float scale;       /* softmax scale on q.k; 0 selects 1/sqrt(d/maps) */
+  int32_t n;         /* new tokens per sample of the attention calls (0 is taken as 1) */
+  int32_t kv_type;   /* BIFATTN_KV_BF16, BIFATTN_KV_FP8_E4M3 or BIFATTN_KV_MXFP4 */
+  int32_t maps;      /* softmax maps of a head: 1 (0 is taken as 1), or 2 for differential heads */
+} bifattn_paged_dims_t;
+
+typedef struct bifattn_paged_plan_s *bifattn_paged_plan_t;
+
+/*
+ * Validate dims and allocate the plan and its workspace on the current HIP
+ * device. Ownership, concurrency and asynchrony are those of bifattn_plan_t:
+ * one plan is not used by two calls that may run at the same time, two
+ * captured graphs' replays included. Errors: EINVAL; EUNSUPPORTED (d, page,
+ * kv_type int8 or int4, maps*(h/g)*n > 64, sequences past 2^30 rows); ENOMEM;
+ * EHIP.
+ */
+bifattn_status_t bifattn_paged_plan_create(const bifattn_paged_dims_t *dims,
+                                           bifattn_paged_plan_t *plan);
+/* As bifattn_plan_destroy. */
+bifattn_status_t bifattn_paged_plan_destroy(bifattn_paged_plan_t plan);
+/* As bifattn_plan_get_info (path is always BIFATTN_PATH_BIFURCATED). */
+bifattn_status_t bifattn_paged_plan_get_info(bifattn_paged_plan_t plan, bifattn_plan_info_t *info);
+/* Synchronise `stream`, then report and clear the plan's device-side flags:
+ * BIFATTN_EPAGE, else BIFATTN_ESCALE, else BIFATTN_ELENS (a length or count
+ * outside its range, clamped, or rows that did not fit), else BIFATTN_OK. */
+bifattn_status_t bifattn_paged_plan_status(bifattn_paged_plan_t plan, hipStream_t stream);
+
+/* New tokens for bifattn_paged_append. Strides count elements between
+ * consecutive samples, heads (groups) and tokens, so that q, k and v may be
+ * parts of one projection's output; elements of a row are consecutive. */
+typedef struct {
+  int32_t samples;  /* sequences the tokens go to: 1..b (context: 1) */
+  int32_t n;        /* tokens per sequence, >= 1 */
+  int32_t context;  /* 0: the samples' own rows; 1: the shared context's */
+  int32_t rot;      /* rotated elements of a head (of each half with maps = 2): a multiple of 16
+                       up to d/maps; 0: none */
+  int32_t neighbours; /* pairs that rotate together: 0: (j, j + rot/2), 1: (2j, 2j + 1) */
+  const int32_t *counts; /* device [samples], valid tokens 0..n of each, or NULL: n */
+  const float *freqs;    /* device [rot/2], radians per position */
+  const void *q;         /* bf16 queries, h heads, or NULL */
+  const void *k, *v;     /* bf16 keys and values, g heads */
+  int64_t q_stride[3], k_stride[3], v_stride[3];
+  void *q_out;           /* bf16 [samples][h][n][d], contiguous; with q only */
+} bifattn_new_rows_t;
+
+/*
+ * Append: token r < counts[i] of sequence i becomes its row lens[i] + r.
+ *   angle_j = position * freqs[j], position = row (context) or m_c + row (own)
+ *   (x, y) -> (x cos - y sin, x sin + y cos) for each pair of q and k; v is not rotated
+ * The rotation is computed in 64 bits from the exact angle, at any position,
+ * and every element is rounded once: q_out and bf16 rows to bf16; fp8 codes
+ * from x / scale, saturated at +-448; an MXFP4 block of 32 elements to the
+ * scale 2^(floor(log2(largest)) - 2) (exponent within [-126, 127]) and the
+ * nearest E2M1 values, ties to even, saturated at 6; a block that holds an
+ * infinity or a NaN becomes NaN. q may overlap nothing that is written.
+ *   lens_out[i] = lens[i] + counts[i]
+ * lens_out may be lens (advanced in place). Rows past the sequence's capacity
+ * (m_c or m_d_max) are dropped, the length stops there, a length outside its
+ * range is clamped first; all raise the ELENS flag. q_out rows of tokens past
+ * counts[i] are left as they were. table [samples][ceil(capacity / page)].
+ * Two sequences of one call must not name the same page.
+ * Errors: EINVAL (null argument, sizes, a stream of another device), EALIGN (a
+ * row not 16-byte aligned), EUNSUPPORTED (rot), EHIP.
+ */
+bifattn_status_t bifattn_paged_append(bifattn_paged_plan_t plan, const bifattn_pages_t *pages,
+                                      const int32_t *table, const bifattn_new_rows_t *rows,
+                                      const int32_t *lens, int32_t *lens_out, hipStream_t stream);
+
+/*
+ * Read rows out: k_out, v_out bf16 [samples][g][rows][d] receive rows first[i]
+ * .. first[i] + rows - 1 of each sequence (first NULL: 0), decoded and rounded
+ * to bf16 once (exact for bf16 and MXFP4). Rows at or past lens[i] are left as
+ * they were. samples 1..b; context and table as in bifattn_paged_append.
+ */
+bifattn_status_t bifattn_paged_gather(bifattn_paged_plan_t plan, const bifattn_pages_t *pages,
+                                      const int32_t *table, const int32_t *first,
+                                      const int32_t *lens, int32_t samples, int32_t rows,
+                                      int32_t context, void *k_out, void *v_out,
+                                      hipStream_t stream);
+
+/*
+ * One decode-attention step over the pages (maps = 1):
+ *   out[i, j, r, :] = softmax_t(scale * q[i,j,r,:] . K_i[t,:]) @ V_i
+ * with K_i the context rows and own rows t < lens[i] - n + r + 1, V_i likewise;
+ * 0 where a token sees no key at all. q bf16 [b][h][n][d]; out bf16, the same
+ * shape, rounded once (the weights enter the value product with 16 bits).
+ * ctx_table [ceil(m_c / page)], tables [b][ceil(m_d_max / page)]; ctx_table may
+ * be NULL only when m_c = 0, tables and lens only when m_d_max = 0.
+ * Errors: EINVAL (null argument, plan with maps = 2, another device's stream),
+ * EALIGN (q, out or a pool tensor not 16-byte aligned, int32 and fp32 ones
+ * 4-byte), EHIP.
+ */
+bifattn_status_t bifattn_paged_decode(bifattn_paged_plan_t plan, const void *q,
+                                      const bifattn_pages_t *pages, const int32_t *ctx_table,
+                                      const int32_t *tables, const int32_t *lens, void *out,
+                                      hipStream_t stream);
+
+/*
+ * Differential attention (maps = 2): a head's q and k rows are two halves of
+ * d/2, each with a softmax map of its own over the same value rows of d:
+ *   y = (softmax(scale * q1 . K1) - lambda[j] * softmax(scale * q2 . K2)) @ V
+ *   out = out_scale * y,  or with weight (fp32 [d]):
+ *   out = out_scale * weight * y / sqrt(mean(y^2) + eps)
+ * lambda: fp32 [h]; eps >= 0. Everything else as in bifattn_paged_decode.
+ */
+bifattn_status_t bifattn_paged_decode_diff(bifattn_paged_plan_t plan, const void *q,
+                                           const bifattn_pages_t *pages, const int32_t *ctx_table,
+                                           const int32_t *tables, const int32_t *lens,
+                                           const float *lambda, const float *weight, float eps,
+                                           float out_scale, void *out, hipStream_t stream);
 
 /* Static text for a status code. Never NULL. */
 const char *bifattn_status_string(bifattn_status_t status);

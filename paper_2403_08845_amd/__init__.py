@@ -18,17 +18,21 @@ import importlib.machinery
 import importlib.util
 import os
 import warnings
+from typing import NamedTuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbifattn.so")
 BIND_PATH = os.path.join(_HERE, "_bifattn_bind.so")
 
 OK, EINVAL, EUNSUPPORTED, EALIGN, ENOMEM, EHIP, ELENS, ESCALE, ESCRATCH = 0, -1, -2, -3, -4, -5, -6, -7, -8
+EPAGE = -9
 #: Size of the fixed device scratch of bifattn_decode_noalloc (BIFATTN_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 64 << 20
 KERNEL_PARTIALS, KERNEL_COMBINE, KERNEL_CALL, KERNEL_CONTEXT, KERNEL_DECODE = 0, 1, 2, 3, 4
 #: Cache element types (bifattn_kv_type_t).
 KV_TYPES = {"bf16": 0, "fp8_e4m3": 1, "int8": 2, "int4": 3}
+#: Element types of paged caches.
+PAGED_KV_TYPES = {"bf16": 0, "fp8_e4m3": 1, "mxfp4": 4}
 #: Paths of bifattn_decode (bifattn_path_t): "auto" lets the plan choose.
 PATHS = {"auto": 0, "bifurcated": 1, "standard": 2}
 
@@ -38,6 +42,9 @@ EXPORTED = (
     "bifattn_append_kv", "bifattn_plan_status", "bifattn_plan_set_timing",
     "bifattn_plan_read_timing", "bifattn_status_string", "bifattn_version",
     "bifattn_decode_noalloc",
+    "bifattn_paged_plan_create", "bifattn_paged_plan_destroy", "bifattn_paged_plan_get_info",
+    "bifattn_paged_plan_status", "bifattn_paged_append", "bifattn_paged_gather",
+    "bifattn_paged_decode", "bifattn_paged_decode_diff",
 )
 
 
@@ -65,6 +72,26 @@ class PlanInfo(ctypes.Structure):
 
     def as_dict(self):
         return {name: getattr(self, name) for name, _ in self._fields_}
+
+
+class PagedDims(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int32), ("h", ctypes.c_int32), ("g", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("m_c", ctypes.c_int32), ("m_d_max", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("n", ctypes.c_int32), ("kv_type", ctypes.c_int32), ("maps", ctypes.c_int32)]
+
+
+class _PagesC(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("K", "V", "K_exp", "V_exp", "k_scale", "v_scale")]
+
+
+class _NewRows(ctypes.Structure):
+    _fields_ = [("samples", ctypes.c_int32), ("n", ctypes.c_int32), ("context", ctypes.c_int32),
+                ("rot", ctypes.c_int32), ("neighbours", ctypes.c_int32), ("counts", ctypes.c_void_p),
+                ("freqs", ctypes.c_void_p), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 3),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+                ("q_out", ctypes.c_void_p)]
 
 
 _lib = None
@@ -97,6 +124,16 @@ def lib() -> ctypes.CDLL:
         L.bifattn_plan_status.argtypes = [vp, vp]
         L.bifattn_plan_set_timing.argtypes = [vp, st, i32]
         L.bifattn_plan_read_timing.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_double)]
+        ppages = ctypes.POINTER(_PagesC)
+        L.bifattn_paged_plan_create.argtypes = [ctypes.POINTER(PagedDims), ctypes.POINTER(vp)]
+        L.bifattn_paged_plan_destroy.argtypes = [vp]
+        L.bifattn_paged_plan_get_info.argtypes = [vp, ctypes.POINTER(PlanInfo)]
+        L.bifattn_paged_plan_status.argtypes = [vp, vp]
+        L.bifattn_paged_append.argtypes = [vp, ppages, vp, ctypes.POINTER(_NewRows), vp, vp, vp]
+        L.bifattn_paged_gather.argtypes = [vp, ppages, vp, vp, vp, i32, i32, i32, vp, vp, vp]
+        L.bifattn_paged_decode.argtypes = [vp, vp, ppages, vp, vp, vp, vp, vp]
+        f32 = ctypes.c_float
+        L.bifattn_paged_decode_diff.argtypes = [vp, vp, ppages, vp, vp, vp, vp, vp, f32, f32, vp, vp]
         L.bifattn_status_string.argtypes = [st]
         L.bifattn_status_string.restype = ctypes.c_char_p
         L.bifattn_version.restype = i32
@@ -459,3 +496,229 @@ def bifattn_plan_read_timing(plan: Plan):
     _check(lib().bifattn_plan_read_timing(plan.handle, ctypes.byref(n), ctypes.byref(ms)),
            "bifattn_plan_read_timing")
     return int(n.value), float(ms.value)
+
+
+class Pages(NamedTuple):
+    """A pool of pages: K, V [num_pages, g, page, d] of the cache type (MXFP4:
+    uint8, last axis d/2, and scale bytes K_exp, V_exp [num_pages, g, page,
+    d/32]); fp8 pools may have group scales k_scale, v_scale, fp32 [g]."""
+    K: object
+    V: object
+    K_exp: object = None
+    V_exp: object = None
+    k_scale: object = None
+    v_scale: object = None
+
+
+class PagedPlan:
+    """A bifattn_paged_plan_t: dimensions of the sequences and of their pool,
+    plus the workspace it owns (n = new tokens per sample of the attention
+    calls; kv = a PAGED_KV_TYPES name; maps = 2 for differential heads)."""
+
+    def __init__(self, b, h, g, d, m_c, m_d_max, page=64, num_pages=1, scale=0.0, n=1, kv="bf16",
+                 maps=1):
+        if kv not in PAGED_KV_TYPES:
+            raise ValueError(f"kv must be one of {sorted(PAGED_KV_TYPES)}")
+        self.kv = kv
+        self.dims = PagedDims(b, h, g, d, m_c, m_d_max, page, num_pages, scale, n,
+                              PAGED_KV_TYPES[kv], maps)
+        handle = ctypes.c_void_p()
+        _check(lib().bifattn_paged_plan_create(ctypes.byref(self.dims), ctypes.byref(handle)),
+               "bifattn_paged_plan_create")
+        self.handle = handle
+        #: As Plan.device.
+        self.device = _torch().device("cuda", _torch().cuda.current_device())
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and self.handle.value:
+            _check(lib().bifattn_paged_plan_destroy(self.handle), "bifattn_paged_plan_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def info(self) -> dict:
+        info = PlanInfo()
+        _check(lib().bifattn_paged_plan_get_info(self.handle, ctypes.byref(info)),
+               "bifattn_paged_plan_get_info")
+        return info.as_dict()
+
+    def empty_pages(self, k_scale=None, v_scale=None) -> Pages:
+        """A pool of this plan's size, zeroed (every stored row is 0)."""
+        torch, D = _torch(), self.dims
+        dt, cols = (torch.bfloat16, D.d) if self.kv == "bf16" else (torch.uint8, _page_cols(D))
+        K, V = (torch.zeros(D.num_pages, D.g, D.page, cols, dtype=dt, device=self.device)
+                for _ in range(2))
+        exps = (None, None)
+        if self.kv == "mxfp4":
+            exps = [torch.zeros(D.num_pages, D.g, D.page, D.d // 32, dtype=torch.uint8,
+                                device=self.device) for _ in range(2)]
+        return Pages(K, V, *exps, k_scale, v_scale)
+
+
+def _page_cols(D):
+    """Last axis of a pool tensor."""
+    return D.d // 2 if D.kv_type == PAGED_KV_TYPES["mxfp4"] else D.d
+
+
+def _ptr_or_none(t, *check):
+    return ctypes.c_void_p(None) if t is None else _tensor(t, *check)
+
+
+def _pages(plan, pages):
+    torch, D, dev = _torch(), plan.dims, plan.device
+    mx = plan.kv == "mxfp4"
+    cd = {"bf16": torch.bfloat16, "fp8_e4m3": (torch.uint8, torch.int8, torch.float8_e4m3fn),
+          "mxfp4": (torch.uint8, torch.int8)}[plan.kv]
+    if not isinstance(pages, Pages):
+        raise TypeError("pages must be a Pages")
+    if (pages.K_exp is None) == mx or (pages.V_exp is None) == mx:
+        raise ValueError("K_exp and V_exp belong to mxfp4 pools")
+    if plan.kv != "fp8_e4m3" and not (pages.k_scale is None and pages.v_scale is None):
+        raise ValueError("k_scale and v_scale belong to fp8_e4m3 pools")
+    shape = (D.num_pages, D.g, D.page, _page_cols(D))
+    eshape = (D.num_pages, D.g, D.page, D.d // 32)
+    return ctypes.byref(_PagesC(
+        _tensor(pages.K, shape, cd, dev, "pages.K"), _tensor(pages.V, shape, cd, dev, "pages.V"),
+        _ptr_or_none(pages.K_exp, eshape, torch.uint8, dev, "pages.K_exp"),
+        _ptr_or_none(pages.V_exp, eshape, torch.uint8, dev, "pages.V_exp"),
+        _ptr_or_none(pages.k_scale, (D.g,), torch.float32, dev, "pages.k_scale"),
+        _ptr_or_none(pages.v_scale, (D.g,), torch.float32, dev, "pages.v_scale")))
+
+
+def _table_shape(D, samples, context):
+    return (samples, -(-(D.m_c if context else D.m_d_max) // D.page))
+
+
+def _rows(t, heads, samples, n, d, device, name):
+    """Device pointer and strides of new rows [samples, heads, n, d], any
+    strides whose rows of d are consecutive and 16-byte aligned."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if tuple(t.shape) != (samples, heads, n, d):
+        raise ValueError(f"{name} must have shape {(samples, heads, n, d)}, got {tuple(t.shape)}")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must live on {device}")
+    if t.stride(3) != 1 or t.is_conj() or t.is_neg():
+        raise ValueError(f"{name} must have consecutive elements in a row")
+    return ctypes.c_void_p(t.data_ptr()), (ctypes.c_int64 * 3)(*(s if e > 1 else 0 for s, e in zip(t.stride(), t.shape[:3])))
+
+
+def bifattn_paged_append(plan: PagedPlan, pages: Pages, table, lens, k, v, lens_out, *, q=None,
+                         q_out=None, counts=None, freqs=None, neighbours=False, context=False,
+                         stream=None):
+    """Enqueue the append of new tokens (see include/bifattn.h): k, v bf16
+    [s, g, n, d] become rows lens[i] .. lens[i] + counts[i] - 1 (counts None:
+    n each) of the s sequences that table int32 [s, pages] names (context: the
+    shared context, s = 1). With freqs (fp32 [rot/2]) keys and queries are
+    rotated to their positions; q bf16 [s, h, n, d] goes to q_out, contiguous.
+    k, v and q may be strided. lens_out int32 [s] receives the new lengths and
+    may be lens."""
+    torch, D, dev = _torch(), plan.dims, plan.device
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise TypeError("k must be a torch.Tensor [samples, g, n, d]")
+    s, n = int(k.shape[0]), int(k.shape[2])
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if freqs is not None and (not isinstance(freqs, torch.Tensor) or freqs.dim() != 1):
+        raise TypeError("freqs must be a torch.Tensor [rot/2]")
+    for out, what in ((q_out, "q_out"), (lens_out, "lens_out")):
+        if isinstance(out, torch.Tensor) and (out.is_conj() or out.is_neg()):
+            raise ValueError(f"{what} must be an ordinary tensor")
+    i32 = torch.int32
+    kp, ks = _rows(k, D.g, s, n, D.d, dev, "k")
+    vp, vs = _rows(v, D.g, s, n, D.d, dev, "v")
+    qp, qs = (ctypes.c_void_p(None), (ctypes.c_int64 * 3)()) if q is None else _rows(q, D.h, s, n, D.d, dev, "q")
+    half = 0 if freqs is None else int(freqs.shape[0])
+    rows = _NewRows(s, n, int(bool(context)), 2 * half, int(bool(neighbours)),
+                    _ptr_or_none(counts, (s,), i32, dev, "counts"),
+                    _ptr_or_none(freqs, (half,), torch.float32, dev, "freqs"), qp, kp, vp, qs, ks, vs,
+                    _ptr_or_none(q_out, (s, D.h, n, D.d), torch.bfloat16, dev, "q_out"))
+    _check(lib().bifattn_paged_append(
+        plan.handle, _pages(plan, pages), _tensor(table, _table_shape(D, s, context), i32, dev, "table"),
+        ctypes.byref(rows), _tensor(lens, (s,), i32, dev, "lens"),
+        _tensor(lens_out, (s,), i32, dev, "lens_out"), _stream_ptr(stream, dev)), "bifattn_paged_append")
+
+
+def bifattn_paged_gather(plan: PagedPlan, pages: Pages, table, lens, k_out, v_out, *, first=None,
+                         context=False, stream=None):
+    """Enqueue the read-out of rows first[i] .. (first None: 0) of each sequence
+    as bf16 into k_out, v_out [s, g, rows, d]; rows at or past lens[i] are left
+    as they were."""
+    torch, D, dev = _torch(), plan.dims, plan.device
+    if not isinstance(k_out, torch.Tensor) or k_out.dim() != 4:
+        raise TypeError("k_out must be a torch.Tensor [samples, g, rows, d]")
+    s, rows = int(k_out.shape[0]), int(k_out.shape[2])
+    shape, i32 = (s, D.g, rows, D.d), torch.int32
+    outs = [_tensor(t, shape, torch.bfloat16, dev, name) for t, name in ((k_out, "k_out"), (v_out, "v_out"))]
+    _check(lib().bifattn_paged_gather(
+        plan.handle, _pages(plan, pages), _tensor(table, _table_shape(D, s, context), i32, dev, "table"),
+        _ptr_or_none(first, (s,), i32, dev, "first"), _tensor(lens, (s,), i32, dev, "lens"), s, rows,
+        int(bool(context)), *outs, _stream_ptr(stream, dev)), "bifattn_paged_gather")
+
+
+def _attention_args(plan, q, ctx_table, tables, lens, out):
+    torch, D, dev = _torch(), plan.dims, plan.device
+    i32 = torch.int32
+    ctx = [(_table_shape(D, 1, True)[1],), _table_shape(D, 1, True)]
+    qp = _tensor(q, _query_shapes(D), torch.bfloat16, dev, "q")
+    return (qp, ctypes.c_void_p(None) if D.m_c == 0 else _tensor(ctx_table, ctx, i32, dev, "ctx_table"),
+            ctypes.c_void_p(None) if D.m_d_max == 0 else
+            _tensor(tables, _table_shape(D, D.b, False), i32, dev, "tables"),
+            ctypes.c_void_p(None) if D.m_d_max == 0 else _tensor(lens, (D.b,), i32, dev, "lens"),
+            _tensor(out, [tuple(q.shape)], torch.bfloat16, dev, "out"))
+
+
+def bifattn_paged_decode(plan: PagedPlan, q, pages: Pages, ctx_table, tables, lens, out, stream=None):
+    """Enqueue one decode-attention step over the pages (see include/bifattn.h):
+    q bf16 [b,h,n,d] ([b,h,d] when n = 1), ctx_table int32 [pages] of the shared
+    context, tables int32 [b, pages] and lens int32 [b] of the own rows; out
+    bf16 shaped like q."""
+    qp, ct, tb, ln, op = _attention_args(plan, q, ctx_table, tables, lens, out)
+    _check(lib().bifattn_paged_decode(plan.handle, qp, _pages(plan, pages), ct, tb, ln, op,
+                                      _stream_ptr(stream, plan.device)), "bifattn_paged_decode")
+
+
+def bifattn_paged_decode_diff(plan: PagedPlan, q, pages: Pages, ctx_table, tables, lens, lam, out, *,
+                              weight=None, eps=1e-5, out_scale=1.0, stream=None):
+    """Enqueue one step of differential attention (plans with maps = 2): lam
+    fp32 [h], weight fp32 [d] or None (heads are not normalised)."""
+    torch, D, dev = _torch(), plan.dims, plan.device
+    qp, ct, tb, ln, op = _attention_args(plan, q, ctx_table, tables, lens, out)
+    _check(lib().bifattn_paged_decode_diff(
+        plan.handle, qp, _pages(plan, pages), ct, tb, ln, _tensor(lam, (D.h,), torch.float32, dev, "lam"),
+        _ptr_or_none(weight, (D.d,), torch.float32, dev, "weight"), float(eps), float(out_scale), op,
+        _stream_ptr(stream, dev)), "bifattn_paged_decode_diff")
+
+
+def bifattn_paged_plan_status(plan: PagedPlan, stream=None) -> int:
+    """Synchronise the stream; return OK, EPAGE, ESCALE or ELENS (and clear the flags)."""
+    st = lib().bifattn_paged_plan_status(plan.handle, _stream_ptr(stream, plan.device))
+    if st not in (OK, EPAGE, ESCALE, ELENS):
+        raise BifattnError(st, "bifattn_paged_plan_status")
+    return st
+
+
+def bifattn_paged_plan_create(b, h, g, d, m_c, m_d_max, page=64, num_pages=1, scale=0.0, n=1,
+                              kv="bf16", maps=1) -> PagedPlan:
+    return PagedPlan(b, h, g, d, m_c, m_d_max, page, num_pages, scale, n, kv, maps)
+
+
+def bifattn_paged_plan_destroy(plan: PagedPlan):
+    plan.close()
+
+
+def bifattn_paged_plan_get_info(plan: PagedPlan) -> dict:
+    return plan.info()

@@ -22,13 +22,16 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libbifattn.so")
-SOURCES = [os.path.join(CSRC, "bifattn_kernels.hip"), os.path.join(CSRC, "bifattn_host.cpp")]
+SOURCES = [os.path.join(CSRC, name) for name in
+           ("bifattn_kernels.hip", "bifattn_paged.hip", "bifattn_paged_rows.hip", "bifattn_host.cpp",
+            "bifattn_paged_host.cpp")]
 BIND_SRC = os.path.join(CSRC, "bifattn_bind.cpp")
 BIND = os.path.join(HERE, "_bifattn_bind.so")
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "-parallel-jobs=4",  # the sources side by side
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # MFMA accumulators in ordinary VGPRs: the online-softmax rescale works on
     # them with VALU ops, which cannot address AGPRs.

@@ -643,6 +643,7 @@ const char* bifattn_status_string(bifattn_status_t s) {
     case BIFATTN_ESCRATCH:
       return "the workspace of this problem exceeds the fixed scratch buffer of "
              "bifattn_decode_noalloc (64 MiB)";
+    case BIFATTN_EPAGE: return "a page id was outside the pool";
   }
   return "unknown status";
 }

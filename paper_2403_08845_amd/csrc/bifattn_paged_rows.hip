@@ -1,0 +1,330 @@
+// Rows in and out of paged caches for gfx950: the append of new tokens (the
+// position rotation of queries and keys, the encoding of keys and values, the
+// scatter into pages) and the read-out of rows as bf16.
+#include <hip/hip_ext.h>
+
+#include "bifattn_device.h"
+#include "bifattn_paged.h"
+
+namespace bifattn {
+namespace {
+
+constexpr int kAppendThreads = 256;
+
+// x rounded to odd: to fp32 toward zero, with the last bit set when anything
+// was cut off. Rounding that to a type of at most 22 significant bits gives
+// the rounding of x itself, ties and borders included.
+__device__ __forceinline__ float odd_f32(double x) {
+  const float f = (float)x;
+  const double back = (double)f;
+  if (back == x || !(fabs(x) <= 3.4e38)) return f;
+  const uint32_t u = __float_as_uint(f) - (fabs(back) > fabs(x) ? 1u : 0u);
+  return __uint_as_float(u | 1u);
+}
+
+// Four words of two bf16 from 8 values.
+__device__ __forceinline__ u32x4 to_bf16(const double* x) {
+  u32x4 r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) r[w] = pack_bf16(odd_f32(x[2 * w]), odd_f32(x[2 * w + 1]));
+  return r;
+}
+
+// Eight OCP E4M3 codes of x / scale, saturated at +-448 (NaN stays NaN).
+__device__ __forceinline__ u32x2 to_fp8(const double* x, double inv) {
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float y = odd_f32(x[e] * inv);
+    f[e] = y > 448.f ? 448.f : (y < -448.f ? -448.f : y);
+  }
+  u32x2 r;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * w], f[4 * w + 1], 0, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * w + 2], f[4 * w + 3], v, true);
+    r[w] = (uint32_t)v;
+  }
+  return r;
+}
+
+// Biased exponent (that of a 64-bit number) of the largest of 8 magnitudes:
+// 0x7ff when one is not finite.
+__device__ __forceinline__ int top_exponent(const double* x) {
+  int t = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t = max(t, (int)((__double_as_longlong(x[e]) >> 52) & 0x7ff));
+  return t;
+}
+// Scale byte of a block whose largest magnitude has that exponent: 2^(byte -
+// 127) with byte - 127 = floor(log2(largest)) - 2 within [-126, 127] (the
+// largest E2M1 value is 1.5 * 2^2), 255 for a block that is not finite.
+__device__ __forceinline__ uint32_t scale_byte(int top) {
+  return top == 0x7ff ? 255u : (uint32_t)min(254, max(1, top - 1023 - 2 + 127));
+}
+// Eight E2M1 codes of x 2^(127 - byte), to nearest even, saturated at 6.
+__device__ __forceinline__ uint32_t to_mx4(const double* x, uint32_t byte) {
+  const float s = __uint_as_float(byte << 23);
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[0]), odd_f32(x[1]), s, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[2]), odd_f32(x[3]), s, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[4]), odd_f32(x[5]), s, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[6]), odd_f32(x[7]), s, 3);
+  return r;
+}
+
+__device__ __forceinline__ void widen8(const u32x4& r, double* x) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    x[2 * w] = __uint_as_float(r[w] << 16);
+    x[2 * w + 1] = __uint_as_float(r[w] & 0xffff0000u);
+  }
+}
+
+// Append. Work-group: sample i, tokens_per_block tokens, heads_per_block of the
+// h query rows, g key rows and g value rows of each. A row is d/16 threads'
+// work, each two chunks of 8 elements that rotate with each other.
+//
+// The angle of a pair is position * freq in 64 bits (positions reach 2^31 and
+// an fp32 product is off by 2^-24 of a turn per turn: 0.06 of a radian at 10^6),
+// formed once per token and pair and kept in LDS; the rotation is exact to 64
+// bits and each element is rounded once, to its stored type, so that codes next
+// to a border fall on the right side.
+//
+// Byte work where the batch is large; a step of some tokens is one launch's
+// latency (a chain of loads: length, table entry, row).
+template <int D, int KV>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParams A) {
+  constexpr int TPR = D / 16;                       // threads of a row
+  constexpr int ROWS = kAppendThreads / TPR;        // rows in flight
+  constexpr int RB = paged_row_bytes(D, KV), EB = D / kMxBlock;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
+  double2* turn = reinterpret_cast<double2*>(dyn);  // [tokens_per_block][rot/2]: cos, sin
+  __shared__ int tops[ROWS][D / 8];
+  const int per = A.token_blocks * A.head_blocks;
+  const int i = blockIdx.x / per, in = blockIdx.x - i * per;
+  const int tb = in / A.head_blocks, hb = in - tb * A.head_blocks;
+  const int raw = A.lens[i];
+  const int start = raw < 0 ? 0 : min(raw, A.max_rows);
+  const int rawn = A.counts ? A.counts[i] : A.n;
+  const int count = rawn < 0 ? 0 : min(rawn, A.n);
+  const int fit = min(count, A.max_rows - start);
+  if (in == 0 && threadIdx.x == 0 && (raw != start || rawn != count || fit != count)) atomicOr(A.status, kStatusLens);
+  const int t0 = tb * A.tokens_per_block, t1 = min(min(A.n, t0 + A.tokens_per_block), count);
+  const int half = A.rot / 2;
+  for (int k = threadIdx.x; k < (t1 - t0) * half; k += kAppendThreads) {
+    const int t = k / half, j = k - t * half;
+    // turns: the product with 1/(2 pi) and the fraction in 64 bits
+    const double rev = (double)((int64_t)A.position0 + start + t0 + t) * ((double)A.freqs[j] * 0.15915494309189533577);
+    double s, c;
+    sincospi(2.0 * (rev - rint(rev)), &s, &c);
+    turn[k] = double2{c, s};
+  }
+  __syncthreads();  // also: every thread has read lens
+  if (threadIdx.x == 0) {
+    if (A.lens_out != A.lens) {
+      if (in == 0) A.lens_out[i] = start + fit;
+    } else if (per == 1) {
+      A.lens_out[i] = start + fit;
+    } else if (atomicAdd(A.tickets + i, 1) == per - 1) {  // the others have read the length
+      A.tickets[i] = 0;
+      A.lens_out[i] = start + fit;
+    }
+  }
+  const int heads = A.h + 2 * A.g;
+  const int h0 = hb * A.heads_per_block, nh = min(heads, h0 + A.heads_per_block) - h0;
+  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int mask = (1 << A.pool.shift) - 1;
+  const int items = max(0, t1 - t0) * nh;
+  // The chunks of a thread. Within each of the maps parts of a row: `halves`
+  // pairs chunk c with c + rot/16, else both elements of a pair are neighbours.
+  const int part_threads = TPR / A.maps, u = t % part_threads, base = t / part_threads * (D / 8 / A.maps);
+  const int rc = A.rot / 16;  // threads with rotated chunks
+  const bool turns = u < rc;
+  const int c0 = base + (turns && !A.neighbours ? u : 2 * u), c1 = turns && !A.neighbours ? c0 + rc : c0 + 1;
+  for (int first = 0; first < items; first += ROWS) {
+    const int item = first + slot;
+    const bool on = item < items;
+    const int r = on ? item / nh : 0, head = h0 + (on ? item - r * nh : 0);
+    const int token = t0 + r;
+    const bool is_q = head < A.h, is_k = !is_q && head < A.h + A.g;
+    const int gam = is_q ? 0 : (is_k ? head - A.h : head - A.h - A.g);
+    double x[8], y[8];
+    u32x4 rx = {0, 0, 0, 0}, ry = {0, 0, 0, 0};
+    if (on && (!is_q || A.q)) {
+      const int64_t* st = is_q ? A.qs : (is_k ? A.ks : A.vs);
+      const uint16_t* src = (is_q ? A.q : (is_k ? A.k : A.v)) + i * st[0] + (is_q ? head : gam) * st[1] + token * st[2];
+      rx = load16(src + 8 * c0);
+      ry = load16(src + 8 * c1);
+    }
+    widen8(rx, x);
+    widen8(ry, y);
+    if (on && turns && (is_q || is_k)) {
+      const double2* cs = turn + r * half;
+      if (A.neighbours) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double2 a = cs[8 * u + e], b = cs[8 * u + 4 + e];
+          const double lo = x[2 * e], hi = x[2 * e + 1], lo2 = y[2 * e], hi2 = y[2 * e + 1];
+          x[2 * e] = lo * a.x - hi * a.y;
+          x[2 * e + 1] = lo * a.y + hi * a.x;
+          y[2 * e] = lo2 * b.x - hi2 * b.y;
+          y[2 * e + 1] = lo2 * b.y + hi2 * b.x;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const double2 a = cs[8 * u + e];
+          const double lo = x[e], hi = y[e];
+          x[e] = lo * a.x - hi * a.y;
+          y[e] = lo * a.y + hi * a.x;
+        }
+      }
+    }
+    if constexpr (KV == kPagedMxfp4) {  // a block is four chunks, of several threads
+      __syncthreads();
+      tops[slot][c0] = top_exponent(x);
+      tops[slot][c1] = top_exponent(y);
+      __syncthreads();
+    }
+    if (!on) continue;
+    if (is_q) {
+      if (A.q) {
+        uint16_t* dst = A.q_out + (((size_t)i * A.h + head) * A.n + token) * D;
+        *reinterpret_cast<u32x4*>(dst + 8 * c0) = to_bf16(x);
+        *reinterpret_cast<u32x4*>(dst + 8 * c1) = to_bf16(y);
+      }
+      continue;
+    }
+    const int row = start + token;
+    if (token >= fit) continue;
+    const int id = A.table[(size_t)i * A.table_pages + (row >> A.pool.shift)];
+    if ((unsigned)id >= (unsigned)A.pool.num_pages) {
+      if (t == 0) atomicOr(A.status, kStatusPage);
+      continue;
+    }
+    const size_t at = ((size_t)((int64_t)id * A.g + gam) << A.pool.shift) + (row & mask);
+    uint8_t* dst = (is_k ? A.pool.K : A.pool.V) + at * RB;
+    if constexpr (KV == kPagedBf16) {
+      *reinterpret_cast<u32x4*>(dst + 16 * c0) = to_bf16(x);
+      *reinterpret_cast<u32x4*>(dst + 16 * c1) = to_bf16(y);
+    } else if constexpr (KV == kPagedFp8) {
+      const float* sc = is_k ? A.pool.k_scale : A.pool.v_scale;
+      const float s = sc ? sc[gam] : 1.f;
+      if (t == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(A.status, kStatusScale);
+      const double inv = 1.0 / (double)s;
+      *reinterpret_cast<u32x2*>(dst + 8 * c0) = to_fp8(x, inv);
+      *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(y, inv);
+    } else {
+      uint8_t* exps = (is_k ? A.pool.K_exp : A.pool.V_exp) + at * EB;
+      const int b0 = c0 / 4, b1 = c1 / 4;
+      const int* ts = tops[slot];
+      const uint32_t s0 = scale_byte(max(max(ts[4 * b0], ts[4 * b0 + 1]), max(ts[4 * b0 + 2], ts[4 * b0 + 3])));
+      const uint32_t s1 = scale_byte(max(max(ts[4 * b1], ts[4 * b1 + 1]), max(ts[4 * b1 + 2], ts[4 * b1 + 3])));
+      *reinterpret_cast<uint32_t*>(dst + 4 * c0) = to_mx4(x, s0);
+      *reinterpret_cast<uint32_t*>(dst + 4 * c1) = to_mx4(y, s1);
+      if (c0 % 4 == 0) exps[b0] = (uint8_t)s0;
+      if (c1 % 4 == 0) exps[b1] = (uint8_t)s1;
+    }
+  }
+}
+
+// Read-out: a thread's 8 elements of a row, widened (times the group's scale)
+// to bf16. Rows at or past a sample's length are not written.
+template <int D, int KV>
+__global__ __launch_bounds__(256) void gather_kernel(PagedGatherParams P) {
+  constexpr int C = D / 8, RB = paged_row_bytes(D, KV), EB = D / kMxBlock;
+  const int64_t items = (int64_t)P.samples * P.pool.g * P.rows * C;
+  const int mask = (1 << P.pool.shift) - 1;
+  for (int64_t k = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; k < items; k += (int64_t)gridDim.x * blockDim.x) {
+    const int c = (int)(k % C);
+    const int64_t line = k / C;
+    const int r = (int)(line % P.rows);
+    const int unit = (int)(line / P.rows);
+    const int i = unit / P.pool.g, gam = unit - i * P.pool.g;
+    const int raw = P.lens[i], from = P.first ? P.first[i] : 0;
+    const int len = raw < 0 ? 0 : min(raw, P.max_rows);
+    if (c == 0 && r == 0 && gam == 0 && (raw != len || from < 0)) atomicOr(P.status, kStatusLens);
+    const int64_t row = (int64_t)from + r;
+    if (from < 0 || row >= len) continue;
+    const int id = P.table[(size_t)i * P.table_pages + (row >> P.pool.shift)];
+    if ((unsigned)id >= (unsigned)P.pool.num_pages) {
+      if (c == 0) atomicOr(P.status, kStatusPage);
+      continue;
+    }
+    const size_t at = ((size_t)((int64_t)id * P.pool.g + gam) << P.pool.shift) + ((int)row & mask);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint8_t* src = (u ? P.pool.V : P.pool.K) + at * RB;
+      u32x4 w;
+      if constexpr (KV == kPagedBf16) {
+        w = *reinterpret_cast<const u32x4*>(src + 16 * c);
+      } else if constexpr (KV == kPagedFp8) {
+        const u32x2 b = *reinterpret_cast<const u32x2*>(src + 8 * c);
+        const float* sc = u ? P.pool.v_scale : P.pool.k_scale;
+        const float s = sc ? sc[gam] : 1.f;
+        if (c == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(P.status, kStatusScale);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)b[e], false);
+          const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)b[e], true);
+          w[2 * e] = pack_bf16(lo[0] * s, lo[1] * s);
+          w[2 * e + 1] = pack_bf16(hi[0] * s, hi[1] * s);
+        }
+      } else {
+        const uint32_t b = *reinterpret_cast<const uint32_t*>(src + 4 * c);
+        const float s = __uint_as_float((uint32_t)((u ? P.pool.V_exp : P.pool.K_exp) + at * EB)[c / 4] << 23);
+        w = u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, s, 0)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, s, 1)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, s, 2)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, s, 3))};
+      }
+      *reinterpret_cast<u32x4*>((u ? P.v_out : P.k_out) + (size_t)line * D + 8 * c) = w;
+    }
+  }
+}
+
+template <typename Prm>
+hipError_t go(void (*kernel)(Prm), int grid, int block, int lds, hipStream_t stream, hipEvent_t stop, const Prm& p) {
+  if (stop)
+    hipExtLaunchKernelGGL(kernel, dim3(grid), dim3(block), lds, stream, nullptr, stop, 0, p);
+  else
+    kernel<<<grid, block, lds, stream>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedAppendParams& A, int kv, hipStream_t s, hipEvent_t stop) {
+  const int grid = A.samples * A.token_blocks * A.head_blocks;
+  const int lds = A.tokens_per_block * (A.rot / 2) * (int)sizeof(double2);
+  auto run = [&](auto kernel) { return go(kernel, grid, kAppendThreads, lds, s, stop, A); };
+  if (A.d == 128) {
+    if (kv == kPagedBf16) return run(append_kernel<128, kPagedBf16>);
+    if (kv == kPagedFp8) return run(append_kernel<128, kPagedFp8>);
+    if (kv == kPagedMxfp4) return run(append_kernel<128, kPagedMxfp4>);
+  } else if (A.d == 64) {
+    if (kv == kPagedBf16) return run(append_kernel<64, kPagedBf16>);
+    if (kv == kPagedFp8) return run(append_kernel<64, kPagedFp8>);
+    if (kv == kPagedMxfp4) return run(append_kernel<64, kPagedMxfp4>);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_gather(const PagedGatherParams& P, int kv, hipStream_t s, hipEvent_t stop) {
+  const int64_t items = (int64_t)P.samples * P.pool.g * P.rows * (P.d / 8);
+  const int grid = (int)((items + 255) / 256 < 16384 ? (items + 255) / 256 : 16384);
+  auto run = [&](auto kernel) { return go(kernel, grid, 256, 0, s, stop, P); };
+  if (P.d == 128) {
+    if (kv == kPagedBf16) return run(gather_kernel<128, kPagedBf16>);
+    if (kv == kPagedFp8) return run(gather_kernel<128, kPagedFp8>);
+    if (kv == kPagedMxfp4) return run(gather_kernel<128, kPagedMxfp4>);
+  } else if (P.d == 64) {
+    if (kv == kPagedBf16) return run(gather_kernel<64, kPagedBf16>);
+    if (kv == kPagedFp8) return run(gather_kernel<64, kPagedFp8>);
+    if (kv == kPagedMxfp4) return run(gather_kernel<64, kPagedMxfp4>);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace bifattn
