@@ -381,7 +381,7 @@ typedef struct bifattn_paged_plan_s *bifattn_paged_plan_t;
  * device. Ownership, concurrency and asynchrony are those of bifattn_plan_t:
  * one plan is not used by two calls that may run at the same time, two
  * captured graphs' replays included. Errors: EINVAL; EUNSUPPORTED (d, page,
- * kv_type int8 or int4, maps*(h/g)*n > 64, sequences past 2^30 rows); ENOMEM;
+ * kv_type int8 or int4, maps*(h/g)*n > 64, sequences past 2^29 rows); ENOMEM;
  * EHIP.
  */
 bifattn_status_t bifattn_paged_plan_create(const bifattn_paged_dims_t *dims,

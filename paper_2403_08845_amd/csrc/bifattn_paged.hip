@@ -72,6 +72,30 @@ __device__ __forceinline__ u32x4 widen_mx4(uint32_t w, uint32_t e) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)),
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
 }
+// The same to fp16, which holds E4M3 values exactly, and E2M1 values whose
+// scale is within its range.
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ u32x4 widen_fp8_f16(uint32_t a, uint32_t b) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true))};
+}
+__device__ __forceinline__ u32x4 widen_mx4_f16(uint32_t w, uint32_t e) {
+  const float s = __uint_as_float(e << 23);
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3))};
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  f16x2 v = {(_Float16)lo, (_Float16)hi};  // round to nearest even
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ f32x16 mfma32_f16(const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 __device__ __forceinline__ uint32_t load_u8(__amdgpu_buffer_rsrc_t r, int off) {
   return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, off, 0, kAuxStream);
 }
@@ -299,68 +323,69 @@ template <int D, typename KV> struct StreamLds {
 };
 template <int D, int NT> constexpr int q_bytes() { return NT * (D / 32) * 64 * 16; }
 
-// Q^T operands of NT query tiles into LDS [NT][d/32][64 lanes], by the four
-// waves of a unit. row_ptr(r): the bf16 row of tile row r, or null; map_of(r):
-// its map. With maps = 2 a row's other half is zero.
-template <int D, int NT, typename KV, typename RowPtr, typename MapOf>
-__device__ __forceinline__ void stage_queries(unsigned char* qs, RowPtr row_ptr, MapOf map_of, int maps,
-                                              uint32_t sign, int wave, int lane) {
-  constexpr int KS = D / 32;
-  const int n = lane & 15, G = lane >> 4;
-  for (int slot = wave; slot < NT * KS; slot += kWaves) {
-    const int nt = slot / KS, s = slot % KS;
-    const int r = nt * kRowsPerTile + n;
-    const uint16_t* qr = row_ptr(r);
-    const int dim = PageTile<D, KV>::qdim(s, G);
-    const bool on = qr && (maps == 1 || dim / (D / 2) == map_of(r));
-    u32x4 q = {0, 0, 0, 0};
-    if (on) q = load16(qr + dim) ^ sign;
-    write128(qs + (slot * 64 + lane) * 16, q);
-  }
+// Q^T operand slot (nt, s) of a unit: row r = 16nt + n, 8 elements from qdim.
+// ptr(r): the bf16 row of tile row r (any valid row for padding ones: the load
+// is unconditional, so that a slot's loads issue together); on(r): not padding;
+// map(r): its map. With maps = 2 a row's other half is zero.
+template <int D, typename KV, typename Rows>
+__device__ __forceinline__ u32x4 query_slot(const Rows& rows, int nt, int s, int maps, uint32_t sign, int lane) {
+  const int r = nt * kRowsPerTile + (lane & 15), dim = PageTile<D, KV>::qdim(s, lane >> 4);
+  const u32x4 q = load16(rows.ptr(r) + dim) ^ sign;
+  const bool on = rows.on(r) && (maps == 1 || dim / (D / 2) == rows.map(r));
+  u32x4 z;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) z[w] = on ? q[w] : 0u;
+  return z;
 }
 
-// One wave streams the tiles k0, k0 + stride, ... below k1 of one sequence.
-// The page ids of a tile are read two tiles ahead and its rows one tile ahead:
-// the ids of tile t + 2 are requested before the rows of tile t + 1, so the
-// wait for those rows covers them. kend: the end that the tokens' limits count
-// from. Returns whether a page id was outside the pool (read as page 0).
-template <int D, int NT, typename KV>
+// Page ids of the halves of the 32-key tile at `key`: lane 0 the first's, lane
+// 1 the second's. Rows from `end` (> 0) on have no entry of their own.
+__device__ __forceinline__ int tile_ids(const int32_t* table, int key, int end, int shift, int lane) {
+  return table[min(key + 16 * (lane & 1), end - 1) >> shift];
+}
+
+// One wave streams the tiles k0, k0 + stride, ... below k1 of one sequence;
+// ids0, ids1 are the first two tiles' ids. DEPTH tiles are in flight: a bf16
+// tile is 16 KB a wave, enough at one; of codes, four (two) times smaller, two
+// (measured on 32 samples of an MHA layer over 8k, MXFP4). A tile's ids are
+// requested an iteration before its rows, ahead of rows that are waited for
+// anyway. kend: the end that the tokens' limits count from. Returns whether a
+// page id was outside the pool (read as page 0).
+template <int D, int NT, typename KV, typename QAt>
 __device__ __forceinline__ bool stream_pages(PageState<D, NT>& st, const PagePool& P, int gam,
-                                             const int32_t* table, const unsigned char* qs,
-                                             unsigned char* kl, unsigned char* vl, int k0, int k1, int kend,
+                                             const int32_t* table, QAt&& q_at, unsigned char* kl,
+                                             unsigned char* vl, int ids0, int ids1, int k0, int k1, int kend,
                                              int stride, int ntok, float scale_log2, int lane) {
-  constexpr int KS = D / 32;
-  if (k0 >= k1) return false;
+  constexpr int DEPTH = KV::BITS == 16 ? 1 : 2;
   bool bad = false;
-  auto get_ids = [&](int key) {  // lane 0: the first half's page, lane 1: the second's
-    return table[min(key + 16 * (lane & 1), k1 - 1) >> P.shift];
+  if (k0 >= k1) return false;
+  PageTile<D, KV> T[DEPTH];
+  auto load = [&](PageTile<D, KV>& t, int ids, int key) {
+    const bool wrong = (unsigned)ids >= (unsigned)P.num_pages;
+    bad |= wrong && key + 16 * (lane & 1) < k1;
+    ids = wrong ? 0 : ids;
+    t.load(P, gam, __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), min(key, k1), k1, lane);
   };
-  auto checked = [&](int id) {
-    const bool wrong = (unsigned)id >= (unsigned)P.num_pages;
-    bad |= wrong;
-    return wrong ? 0 : id;
-  };
-  PageTile<D, KV> A;
-  int ids = checked(get_ids(k0)), next = get_ids(k0 + stride);
-  A.load(P, gam, __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), k0, k1, lane);
-  u32x4 qreg[NT == 1 ? KS : 1];
-  if constexpr (NT == 1) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qreg[s] = read128(qs + (s * 64 + lane) * 16);
+  auto ids_at = [&](int key) { return tile_ids(table, min(key, k1 - 1), k1, P.shift, lane); };
+  load(T[0], ids0, k0);
+  int next = ids1;  // ids of the next tile to load
+  if constexpr (DEPTH == 2) {
+    next = ids_at(k0 + 2 * stride);
+    load(T[1], ids1, k0 + stride);
   }
-  auto q_at = [&](int nt, int s) -> u32x4 {
-    if constexpr (NT == 1) return qreg[s];
-    return *(volatile const lds_u32x4*)(qs + ((nt * KS + s) * 64 + lane) * 16);
-  };
-  for (int key = k0; key < k1; key += stride) {
-    A.stage(kl, vl, lane);
-    ids = checked(next);
-    const int id0 = __builtin_amdgcn_readlane(ids, 0), id1 = __builtin_amdgcn_readlane(ids, 1);
-    next = get_ids(min(key + 2 * stride, k1 - 1));
-    PageTile<D, KV> cur;
-    if constexpr (KV::MX) cur = A;  // K operands come from the registers
-    A.load(P, gam, id0, id1, min(key + stride, k1), k1, lane);
-    page_update(st, KV::MX ? cur : A, kl, vl, q_at, kend - key, ntok, scale_log2, lane);
+  for (int key = k0; key < k1;) {
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u) {
+      T[u].stage(kl, vl, lane);
+      PageTile<D, KV> cur;
+      if constexpr (KV::MX) cur = T[u];  // K operands come from the registers
+      const int ids = next;
+      next = ids_at(key + (DEPTH + 1) * stride);
+      load(T[u], ids, key + DEPTH * stride);
+      page_update(st, KV::MX ? cur : T[u], kl, vl, q_at, kend - key, ntok, scale_log2, lane);
+      key += stride;
+      if (key >= k1) break;
+    }
   }
   return bad;
 }
@@ -374,35 +399,56 @@ template <int D, int NT> __device__ __forceinline__ void total_sums(PageState<D,
 __device__ __forceinline__ float group_scale_log2(const PagedAttnParams& P, int gam) {
   return P.pool.k_scale ? P.scale_log2 * P.pool.k_scale[gam] : P.scale_log2;
 }
-__device__ __forceinline__ int own_len(const PagedAttnParams& P, int i) {
-  const int raw = P.lens ? P.lens[i] : 0;
-  return __builtin_amdgcn_readfirstlane(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
-}
 
 // Own rows: work-group (sample i, group gam, chunk s) of four waves, which take
 // interleaved tiles and write a partial each of the unit's R rows. All waves
-// of the work-group call it (`on`: whether this unit exists).
+// of the work-group call it (`on`: whether this unit exists). The length, the
+// first page ids and the queries are requested together: the ids within the
+// row capacity, whose entries past the length are not used.
+struct OwnRows {
+  const uint16_t* base;
+  int D, R, pn;
+  __device__ __forceinline__ const uint16_t* ptr(int r) const {
+    const int rr = min(r, R - 1);
+    return base + (size_t)(rr < pn ? rr : rr - pn) * D;
+  }
+  __device__ __forceinline__ bool on(int r) const { return r < R; }
+  __device__ __forceinline__ int map(int r) const { return r < pn ? 0 : 1; }
+};
 template <int D, int NT, typename KV>
 __device__ __forceinline__ void own_block(const PagedAttnParams& P, int blk, bool on, int wave, int lane,
                                           unsigned char* qs, unsigned char* kl, unsigned char* vl) {
+  constexpr int KS = D / 32;
+  blk = on ? blk : 0;
   const int s = blk % P.S_d, ig = blk / P.S_d;
   const int gam = ig % P.g, i = ig / P.g;
-  if (on) {
-    const uint16_t* qb = P.q + ((size_t)i * P.hn + (size_t)gam * P.pn) * D;
-    const int R = P.R, pn = P.pn;
-    stage_queries<D, NT, KV>(
-        qs, [&](int r) -> const uint16_t* { return r < R ? qb + (size_t)(r < pn ? r : r - pn) * D : nullptr; },
-        [&](int r) { return r < pn ? 0 : 1; }, P.maps, P.q_sign, wave, lane);
+  const int c0 = s * P.dec_keys, k0 = c0 + wave * kTileKeys, cap = min(P.m_d_max, c0 + P.dec_keys);
+  constexpr int stride = kWaves * kTileKeys;
+  const int32_t* table = P.tables + (size_t)i * P.table_pages;
+  const int ids0 = tile_ids(table, min(k0, cap - 1), cap, P.pool.shift, lane);
+  const int ids1 = tile_ids(table, min(k0 + stride, cap - 1), cap, P.pool.shift, lane);
+  const int raw = P.lens[i];
+  const OwnRows rows = {P.q + ((size_t)i * P.hn + (size_t)gam * P.pn) * D, D, P.R, P.pn};
+  u32x4 qreg[NT == 1 ? KS : 1];
+  if constexpr (NT == 1) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qreg[k] = query_slot<D, KV>(rows, 0, k, P.maps, P.q_sign, lane);
+  } else {
+    for (int k = wave; k < NT * KS; k += kWaves)
+      write128(qs + (k * 64 + lane) * 16, query_slot<D, KV>(rows, k / KS, k % KS, P.maps, P.q_sign, lane));
+    __syncthreads();
   }
-  __syncthreads();
   if (!on) return;
-  const int total = own_len(P, i);
-  const int k0 = s * P.dec_keys;
+  const int total = __builtin_amdgcn_readfirstlane(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
+  auto q_at = [&](int nt, int k) -> u32x4 {
+    if constexpr (NT == 1) return qreg[k];
+    return *(volatile const lds_u32x4*)(qs + ((nt * KS + k) * 64 + lane) * 16);
+  };
   PageState<D, NT> st;
   st.init();
-  const bool bad = stream_pages<D, NT, KV>(st, P.pool, gam, P.tables + (size_t)i * P.table_pages, qs, kl, vl,
-                                           k0 + wave * kTileKeys, min(total, k0 + P.dec_keys), total,
-                                           kWaves * kTileKeys, P.ntok, group_scale_log2(P, gam), lane);
+  const bool bad =
+      stream_pages<D, NT, KV>(st, P.pool, gam, table, q_at, kl, vl, ids0, ids1, k0, min(total, c0 + P.dec_keys), total,
+                              stride, P.ntok, group_scale_log2(P, gam), lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
   const size_t prow = ((size_t)blk * kWaves + wave) * P.R;
@@ -425,6 +471,16 @@ template <int D, int NT> struct PageMerge {
   static constexpr int bytes = (ROWS * LD + 2 * ROWS) * 4;
 };
 
+struct GroupRows {  // row u*Mh + i*pn + jp of a group
+  const uint16_t* base;
+  int D, M, Mh, pn, hn;
+  __device__ __forceinline__ const uint16_t* ptr(int r) const {
+    const int rr = min(r, M - 1), rm = rr < Mh ? rr : rr - Mh, i = rm / pn;
+    return base + ((size_t)i * hn + (rm - i * pn)) * D;
+  }
+  __device__ __forceinline__ bool on(int r) const { return r < M; }
+  __device__ __forceinline__ int map(int r) const { return r < Mh ? 0 : 1; }
+};
 // Context, few rows per group: the 4 S_c waves of a group take its tiles round
 // robin; the four waves' states merge in LDS, in wave order, into the split's
 // partial.
@@ -434,23 +490,28 @@ __device__ __forceinline__ void ctx_few_block(const PagedAttnParams& P, int blk,
                                               float* merge) {
   constexpr int LD = PageMerge<D, NT>::LD, ROWS = PageMerge<D, NT>::ROWS;
   const int s = blk % P.S_c, gam = blk / P.S_c;
-  const int M = P.M, Mh = P.Mh, pn = P.pn, hn = P.hn;
-  const uint16_t* q = P.q + (size_t)gam * pn * D;
-  stage_queries<D, NT, KV>(
-      qs,
-      [&](int r) -> const uint16_t* {
-        if (r >= M) return nullptr;
-        const int rr = r < Mh ? r : r - Mh;
-        const int i = rr / pn;
-        return q + ((size_t)i * hn + (rr - i * pn)) * D;
-      },
-      [&](int r) { return r < Mh ? 0 : 1; }, P.maps, P.q_sign, wave, lane);
+  constexpr int KS = D / 32;
+  const int M = P.M;
+  const int k0 = (s * kWaves + wave) * kTileKeys, stride = P.S_c * kWaves * kTileKeys;
+  const int ids0 = tile_ids(P.ctx_table, min(k0, P.m_c - 1), P.m_c, P.pool.shift, lane);
+  const int ids1 = tile_ids(P.ctx_table, min(k0 + stride, P.m_c - 1), P.m_c, P.pool.shift, lane);
+  const GroupRows rows = {P.q + (size_t)gam * P.pn * D, D, M, P.Mh, P.pn, P.hn};
+  for (int k = wave; k < NT * KS; k += kWaves)
+    write128(qs + (k * 64 + lane) * 16, query_slot<D, KV>(rows, k / KS, k % KS, P.maps, P.q_sign, lane));
   __syncthreads();
+  u32x4 qreg[NT == 1 ? KS : 1];
+  if constexpr (NT == 1) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qreg[k] = read128(qs + (k * 64 + lane) * 16);
+  }
+  auto q_at = [&](int nt, int k) -> u32x4 {
+    if constexpr (NT == 1) return qreg[k];
+    return *(volatile const lds_u32x4*)(qs + ((nt * KS + k) * 64 + lane) * 16);
+  };
   PageState<D, NT> st;
   st.init();
-  const bool bad = stream_pages<D, NT, KV>(st, P.pool, gam, P.ctx_table, qs, kl, vl, (s * kWaves + wave) * kTileKeys,
-                                           P.m_c, P.m_c, P.S_c * kWaves * kTileKeys, 1, group_scale_log2(P, gam),
-                                           lane);
+  const bool bad = stream_pages<D, NT, KV>(st, P.pool, gam, P.ctx_table, q_at, kl, vl, ids0, ids1, k0, P.m_c, P.m_c, stride,
+                                           1, group_scale_log2(P, gam), lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
   float* m_s = merge + ROWS * LD;
@@ -523,6 +584,12 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
 // stage ahead of the products, their page ids two stages ahead; one barrier a
 // stage. With maps = 2 a row block belongs to one map, whose half of the key
 // rows alone enters its logits.
+//
+// Bound by the matrix cores, so code caches take fp16 for the value product:
+// one term of 11 bits for the weights (their error 2e-4 beside the output's
+// 1.7e-3) where bf16 values need two. E4M3 values are exact in fp16. MXFP4
+// values enter relative to the largest scale of the work-group's keys, read
+// ahead (1/16 of the chunk's value bytes), and are exact down to 2^-31 of it.
 template <int D, int NW, int SK, typename KV, int MAPS>
 __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigned char* lds) {
   constexpr int KD = D / MAPS;             // dims of the logits
@@ -545,6 +612,12 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   const PagePool& pool = P.pool;
   const int mask = (1 << pool.shift) - 1;
   bool bad = false;
+  constexpr bool kHalf = KV::BITS < 16;  // values and weights in fp16
+  auto row_of = [&](int key, int id) {  // pool row of a context key, by its page id
+    const bool wrong = (unsigned)id >= (unsigned)pool.num_pages;
+    bad |= wrong;
+    return ((size_t)((int64_t)(wrong ? 0 : id) * pool.g + gam) << pool.shift) + (key & mask);
+  };
 
   // Load u of a thread: 16 bytes, chunk c of row `row` of K (first half of the
   // loads) or V. Rows past the range repeat its last one and are zeroed.
@@ -573,14 +646,12 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
       bool is_v;
       int row, c;
       chunk(u, is_v, row, c);
-      const bool wrong = (unsigned)ids[u] >= (unsigned)pool.num_pages;
-      bad |= wrong;
-      const int key = k0 + min(key0 + row, nkeys - 1);
-      const size_t at = ((size_t)((int64_t)(wrong ? 0 : ids[u]) * pool.g + gam) << pool.shift) + (key & mask);
+      const size_t at = row_of(k0 + min(key0 + row, nkeys - 1), ids[u]);
       reg[u] = *reinterpret_cast<const u32x4*>((is_v ? pool.V : pool.K) + at * RB + 16 * c);
       if constexpr (KV::MX) ex[u] = ((is_v ? pool.V_exp : pool.K_exp) + at * EB)[c];
     }
   };
+  int vref = 0;  // MXFP4: exponent that the scales of the value rows are relative to
   auto stage_put = [&](int key0, int buf) {
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
@@ -593,18 +664,42 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
       if constexpr (KV::BITS == 16) {
         write128(dst, w);
       } else if constexpr (KV::BITS == 8) {
-        write128(dst, widen_fp8(w[0], w[1]));
-        write128(dst + 16, widen_fp8(w[2], w[3]));
+        write128(dst, is_v ? widen_fp8_f16(w[0], w[1]) : widen_fp8(w[0], w[1]));
+        write128(dst + 16, is_v ? widen_fp8_f16(w[2], w[3]) : widen_fp8(w[2], w[3]));
       } else {
-        const uint32_t e = key0 + SK > nkeys && key0 + row >= nkeys ? 0u : ex[u];
+        uint32_t e = key0 + SK > nkeys && key0 + row >= nkeys ? 0u : ex[u];
+        if (is_v) {  // wave-uniform
+          e = e == 255u ? e : (uint32_t)max(0, (int)e - vref);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) write128(dst + 16 * k, widen_mx4(w[k], e));
+          for (int k = 0; k < 4; ++k) write128(dst + 16 * k, widen_mx4_f16(w[k], e));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) write128(dst + 16 * k, widen_mx4(w[k], e));
+        }
       }
     }
   };
   get_ids(0);
   stage_get(0);
   if (SK < nkeys) get_ids(SK);
+  if constexpr (KV::MX) {
+    // the largest scale byte that is a number; values then reach 6 * 2^8
+    int top = 0;
+    for (int key = threadIdx.x; key < nkeys; key += 64 * NW) {
+      const uint8_t* e = pool.V_exp + row_of(k0 + key, P.ctx_table[(k0 + key) >> pool.shift]) * EB;
+#pragma unroll
+      for (int c = 0; c < EB; ++c) top = max(top, e[c] == 255 ? 0 : (int)e[c]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o));
+    int* tops = reinterpret_cast<int*>(lds);
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = max(top, tops[w]);
+    vref = __builtin_amdgcn_readfirstlane(top) - 127 - 8;
+    __syncthreads();
+  }
 
   const int Mh = P.Mh, pn = P.pn;
   const bool active = row0 < Mh;  // wave-uniform
@@ -702,14 +797,24 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
 #pragma unroll
       for (int ss = 0; ss < 2; ++ss) {
         uint32_t hi[4], lo[4];
-        split_weights<4>(pr + 8 * ss, hi, lo);
+        if constexpr (kHalf) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) hi[w] = pack_f16(pr[8 * ss + 2 * w], pr[8 * ss + 2 * w + 1]);
+        } else {
+          split_weights<4>(pr + 8 * ss, hi, lo);
+        }
 #pragma unroll
         for (int t = 0; t < DB; ++t) {
           const unsigned char* p = vb + (32 * b + 16 * ss) * VROW + 64 * t;
           const u32x2 v0 = read_tr(p), v1 = read_tr(p + 8 * VROW);
           const u32x4 v = u32x4{v0[0], v0[1], v1[0], v1[1]};
-          acc[t] = mfma32(v, u32x4{hi[0], hi[1], hi[2], hi[3]}, acc[t]);
-          acc[t] = mfma32(v, u32x4{lo[0], lo[1], lo[2], lo[3]}, acc[t]);
+          const u32x4 first = u32x4{hi[0], hi[1], hi[2], hi[3]};
+          if constexpr (kHalf) {
+            acc[t] = mfma32_f16(v, first, acc[t]);
+          } else {
+            acc[t] = mfma32(v, first, acc[t]);
+            acc[t] = mfma32(v, u32x4{lo[0], lo[1], lo[2], lo[3]}, acc[t]);
+          }
         }
       }
     }
@@ -721,6 +826,12 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   if (row < Mh) {
     const size_t prow = ((size_t)gam * P.S_c + s) * P.M + (size_t)map * Mh + row;
     float* dst = P.ctx_acc + prow * D;
+    if constexpr (KV::MX) {
+#pragma unroll
+      for (int t = 0; t < DB; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vref);
+    }
 #pragma unroll
     for (int t = 0; t < DB; ++t)
 #pragma unroll

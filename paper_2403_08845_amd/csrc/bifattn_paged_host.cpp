@@ -87,7 +87,8 @@ bifattn_status_t check_dims(const bifattn_paged_dims_t* d) {
   if (d->page < 16 || d->page > 256 || (d->page & (d->page - 1))) return BIFATTN_EUNSUPPORTED;
   const double ntok = d->n > 0 ? d->n : 1, maps = d->maps == 2 ? 2 : 1;
   if (maps * (d->h / d->g) * ntok > kMaxP) return BIFATTN_EUNSUPPORTED;
-  if (d->m_c > (1 << 30) || d->m_d_max > (1 << 30)) return BIFATTN_EUNSUPPORTED;
+  // row numbers up to three strides past the end stay within 32 bits
+  if (d->m_c > (1 << 29) || d->m_d_max > (1 << 29)) return BIFATTN_EUNSUPPORTED;
   if (maps * d->b * d->h * ntok > INT32_MAX / 2 || (double)d->b * d->g > INT32_MAX / 2) return BIFATTN_EINVAL;
   if ((double)d->num_pages * d->g * d->page * d->d * 2 > 4.0e18 ||
       (double)d->b * (d->m_c + (double)d->m_d_max) * d->g * d->d > 4.0e18)
