@@ -194,6 +194,28 @@ def _caller(dims, handle, device_index):
                        D.m_c, D.m_d_max, max(1, D.n), D.kv_type)
 
 
+def _paged_caller(dims, handle, device_index):
+    """The native caller of a paged plan's entry points, or None."""
+    bind = _bind_module()
+    if bind is None:
+        return None
+    L = lib()
+    addr = [ctypes.cast(f, ctypes.c_void_p).value for f in
+            (L.bifattn_paged_append, L.bifattn_paged_gather, L.bifattn_paged_decode,
+             L.bifattn_paged_decode_diff)]
+    D = dims
+    return bind.PagedCaller(*addr, handle.value, _raw_stream_getter(), device_index, D.b, D.h, D.g, D.d,
+                            D.m_c, D.m_d_max, max(1, D.n), D.kv_type, D.page, D.num_pages, Pages)
+
+
+def _taken(status, what) -> bool:
+    """Whether the native caller made the call; raises its error."""
+    if status is None:
+        return False
+    _check(status, what)
+    return True
+
+
 def status_string(status: int) -> str:
     return lib().bifattn_status_string(int(status)).decode()
 
@@ -528,8 +550,10 @@ class PagedPlan:
         self.handle = handle
         #: As Plan.device.
         self.device = _torch().device("cuda", _torch().cuda.current_device())
+        self._caller = _paged_caller(self.dims, handle, self.device.index)
 
     def close(self):
+        self._caller = None
         if getattr(self, "handle", None) is not None and self.handle.value:
             _check(lib().bifattn_paged_plan_destroy(self.handle), "bifattn_paged_plan_destroy")
             self.handle = None
@@ -626,6 +650,10 @@ def bifattn_paged_append(plan: PagedPlan, pages: Pages, table, lens, k, v, lens_
     rotated to their positions; q bf16 [s, h, n, d] goes to q_out, contiguous.
     k, v and q may be strided. lens_out int32 [s] receives the new lengths and
     may be lens."""
+    caller = getattr(plan, "_caller", None)
+    if caller is not None and _taken(caller.append(pages, table, lens, k, v, lens_out, q, q_out, counts, freqs, neighbours, context,
+                                            None if stream is None else _stream_ptr(stream).value or 0), "bifattn_paged_append"):
+        return
     torch, D, dev = _torch(), plan.dims, plan.device
     if not isinstance(k, torch.Tensor) or k.dim() != 4:
         raise TypeError("k must be a torch.Tensor [samples, g, n, d]")
@@ -657,6 +685,10 @@ def bifattn_paged_gather(plan: PagedPlan, pages: Pages, table, lens, k_out, v_ou
     """Enqueue the read-out of rows first[i] .. (first None: 0) of each sequence
     as bf16 into k_out, v_out [s, g, rows, d]; rows at or past lens[i] are left
     as they were."""
+    caller = getattr(plan, "_caller", None)
+    if caller is not None and _taken(caller.gather(pages, table, lens, k_out, v_out, first, context,
+                                            None if stream is None else _stream_ptr(stream).value or 0), "bifattn_paged_gather"):
+        return
     torch, D, dev = _torch(), plan.dims, plan.device
     if not isinstance(k_out, torch.Tensor) or k_out.dim() != 4:
         raise TypeError("k_out must be a torch.Tensor [samples, g, rows, d]")
@@ -686,6 +718,10 @@ def bifattn_paged_decode(plan: PagedPlan, q, pages: Pages, ctx_table, tables, le
     q bf16 [b,h,n,d] ([b,h,d] when n = 1), ctx_table int32 [pages] of the shared
     context, tables int32 [b, pages] and lens int32 [b] of the own rows; out
     bf16 shaped like q."""
+    caller = getattr(plan, "_caller", None)
+    if caller is not None and _taken(caller.decode(q, pages, ctx_table, tables, lens, out,
+                                            None if stream is None else _stream_ptr(stream).value or 0), "bifattn_paged_decode"):
+        return
     qp, ct, tb, ln, op = _attention_args(plan, q, ctx_table, tables, lens, out)
     _check(lib().bifattn_paged_decode(plan.handle, qp, _pages(plan, pages), ct, tb, ln, op,
                                       _stream_ptr(stream, plan.device)), "bifattn_paged_decode")
@@ -695,6 +731,10 @@ def bifattn_paged_decode_diff(plan: PagedPlan, q, pages: Pages, ctx_table, table
                               weight=None, eps=1e-5, out_scale=1.0, stream=None):
     """Enqueue one step of differential attention (plans with maps = 2): lam
     fp32 [h], weight fp32 [d] or None (heads are not normalised)."""
+    caller = getattr(plan, "_caller", None)
+    if caller is not None and _taken(caller.diff(q, pages, ctx_table, tables, lens, out, lam, weight, eps, out_scale,
+                                          None if stream is None else _stream_ptr(stream).value or 0), "bifattn_paged_decode_diff"):
+        return
     torch, D, dev = _torch(), plan.dims, plan.device
     qp, ct, tb, ln, op = _attention_args(plan, q, ctx_table, tables, lens, out)
     _check(lib().bifattn_paged_decode_diff(

@@ -441,12 +441,18 @@ bifattn_status_t bifattn_paged_append(bifattn_paged_plan_t P, const bifattn_page
   A.table_pages = (int)ceil_div(A.max_rows, d.page);
   A.position0 = rows->context ? 0 : d.m_c;
   A.samples = rows->samples;
-  // One pass of a work-group (32 rows of 128 elements, 64 of 64) while there
-  // are few tokens, else about four.
+  // A pass of a work-group takes 32 rows of 128 elements (64 of 64). Few tokens:
+  // one pass a work-group. Many: whole tokens, as many (up to 8) as fill their
+  // passes best, while four work-groups per CU remain.
   const int heads = A.h + 2 * A.g, pass = 256 / (d.d / 16);
   const bool many = (int64_t)A.samples * A.n * ceil_div(heads, pass) > 8 * kCUs;
   A.heads_per_block = many ? heads : std::min(heads, pass);
-  A.tokens_per_block = many ? (int)std::min<int64_t>(8, ceil_div(4 * pass, heads)) : 1;
+  A.tokens_per_block = 1;
+  double fill = 0.0;
+  for (int T = 1; many && T <= 8 && (T == 1 || A.samples * ceil_div(A.n, T) >= 4 * kCUs); ++T) {
+    const double f = (double)(T * heads) / (double)round_up(T * heads, pass);
+    if (f > fill + 0.02) fill = f, A.tokens_per_block = T;
+  }
   A.head_blocks = (int)ceil_div(heads, A.heads_per_block);
   const int64_t token_blocks = ceil_div(A.n, A.tokens_per_block);
   if ((double)A.samples * (double)token_blocks * A.head_blocks > INT32_MAX / 2) return BIFATTN_EINVAL;

@@ -22,11 +22,24 @@ __device__ __forceinline__ float odd_f32(double x) {
   return __uint_as_float(u | 1u);
 }
 
-// Four words of two bf16 from 8 values.
+// Four words of two bf16 from 8 values, each rounded once. Going through fp32
+// rounds twice only where the fp32 value lies exactly between two bf16 ones
+// (its low half is 0x8000): those, one in 65536, take the way over odd_f32.
 __device__ __forceinline__ u32x4 to_bf16(const double* x) {
+  float f[8];
+  uint32_t near = 0xffffu;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    f[e] = (float)x[e];
+    near = min(near, (__float_as_uint(f[e]) ^ 0x8000u) & 0xffffu);
+  }
+  if (near == 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = odd_f32(x[e]);
+  }
   u32x4 r;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) r[w] = pack_bf16(odd_f32(x[2 * w]), odd_f32(x[2 * w + 1]));
+  for (int w = 0; w < 4; ++w) r[w] = pack_bf16(f[2 * w], f[2 * w + 1]);
   return r;
 }
 
@@ -49,12 +62,20 @@ __device__ __forceinline__ u32x2 to_fp8(const double* x, double inv) {
 }
 
 // Biased exponent (that of a 64-bit number) of the largest of 8 magnitudes:
-// 0x7ff when one is not finite.
+// 0x7ff when one is not finite. The high words alone order the exponents.
 __device__ __forceinline__ int top_exponent(const double* x) {
-  int t = 0;
+  uint32_t t = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) t = max(t, (int)((__double_as_longlong(x[e]) >> 52) & 0x7ff));
-  return t;
+  for (int e = 0; e < 8; ++e) t = max(t, (uint32_t)__double2hiint(x[e]) & 0x7fffffffu);
+  return (int)(t >> 20);
+}
+// The same of 8 bf16 values as they are stored.
+__device__ __forceinline__ int top_exponent(const u32x4& r) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) t = max(t, max(r[w] & 0x7fffu, (r[w] >> 16) & 0x7fffu));
+  const int e = (int)(t >> 7);
+  return e == 255 ? 0x7ff : e + (t ? 1023 - 127 : 0);  // (bf16 subnormals: below any scale's range)
 }
 // Scale byte of a block whose largest magnitude has that exponent: 2^(byte -
 // 127) with byte - 127 = floor(log2(largest)) - 2 within [-126, 127] (the
@@ -62,25 +83,23 @@ __device__ __forceinline__ int top_exponent(const double* x) {
 __device__ __forceinline__ uint32_t scale_byte(int top) {
   return top == 0x7ff ? 255u : (uint32_t)min(254, max(1, top - 1023 - 2 + 127));
 }
-// Eight E2M1 codes of x 2^(127 - byte), to nearest even, saturated at 6.
-__device__ __forceinline__ uint32_t to_mx4(const double* x, uint32_t byte) {
+// Eight E2M1 codes of f 2^(127 - byte), to nearest even, saturated at 6.
+__device__ __forceinline__ uint32_t to_mx4(const float* f, uint32_t byte) {
   const float s = __uint_as_float(byte << 23);
   uint32_t r = 0;
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[0]), odd_f32(x[1]), s, 0);
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[2]), odd_f32(x[3]), s, 1);
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[4]), odd_f32(x[5]), s, 2);
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, odd_f32(x[6]), odd_f32(x[7]), s, 3);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[0], f[1], s, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[2], f[3], s, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[4], f[5], s, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, f[6], f[7], s, 3);
   return r;
 }
-
-__device__ __forceinline__ void widen8(const u32x4& r, double* x) {
+__device__ __forceinline__ void widen8(const u32x4& r, float* f) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    x[2 * w] = __uint_as_float(r[w] << 16);
-    x[2 * w + 1] = __uint_as_float(r[w] & 0xffff0000u);
+    f[2 * w] = __uint_as_float(r[w] << 16);
+    f[2 * w + 1] = __uint_as_float(r[w] & 0xffff0000u);
   }
 }
-
 // Append. Work-group: sample i, tokens_per_block tokens, heads_per_block of the
 // h query rows, g key rows and g value rows of each. A row is d/16 threads'
 // work, each two chunks of 8 elements that rotate with each other.
@@ -142,58 +161,61 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParam
   const int rc = A.rot / 16;  // threads with rotated chunks
   const bool turns = u < rc;
   const int c0 = base + (turns && !A.neighbours ? u : 2 * u), c1 = turns && !A.neighbours ? c0 + rc : c0 + 1;
+  // The next row's chunks are requested before this row's are worked on.
+  auto fetch = [&](int item, u32x4& rx, u32x4& ry) {
+    const int it = min(item, items - 1), r = it / nh, head = h0 + it - r * nh;
+    const bool is_q = head < A.h, is_k = !is_q && head < A.h + A.g;
+    const int64_t* st = is_q ? A.qs : (is_k ? A.ks : A.vs);
+    const uint16_t* src = (is_q ? A.q : (is_k ? A.k : A.v)) + (int64_t)i * st[0] +
+                          (is_q ? head : (is_k ? head - A.h : head - A.h - A.g)) * st[1] + (t0 + r) * st[2];
+    rx = load16(src + 8 * c0);
+    ry = load16(src + 8 * c1);
+  };
+  if (items == 0) return;
+  u32x4 nx, ny;
+  fetch(slot, nx, ny);
   for (int first = 0; first < items; first += ROWS) {
     const int item = first + slot;
-    const bool on = item < items;
-    const int r = on ? item / nh : 0, head = h0 + (on ? item - r * nh : 0);
-    const int token = t0 + r;
+    const u32x4 rx = nx, ry = ny;
+    if (first + ROWS < items) fetch(item + ROWS, nx, ny);
+    if (item >= items) continue;
+    const int r = item / nh, head = h0 + item - r * nh, token = t0 + r;
     const bool is_q = head < A.h, is_k = !is_q && head < A.h + A.g;
     const int gam = is_q ? 0 : (is_k ? head - A.h : head - A.h - A.g);
     double x[8], y[8];
-    u32x4 rx = {0, 0, 0, 0}, ry = {0, 0, 0, 0};
-    if (on && (!is_q || A.q)) {
-      const int64_t* st = is_q ? A.qs : (is_k ? A.ks : A.vs);
-      const uint16_t* src = (is_q ? A.q : (is_k ? A.k : A.v)) + i * st[0] + (is_q ? head : gam) * st[1] + token * st[2];
-      rx = load16(src + 8 * c0);
-      ry = load16(src + 8 * c1);
-    }
-    widen8(rx, x);
-    widen8(ry, y);
-    if (on && turns && (is_q || is_k)) {
-      const double2* cs = turn + r * half;
-      if (A.neighbours) {
+    if (is_q || is_k) {
+      float fx[8], fy[8];
+      widen8(rx, fx);
+      widen8(ry, fy);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const double2 a = cs[8 * u + e], b = cs[8 * u + 4 + e];
-          const double lo = x[2 * e], hi = x[2 * e + 1], lo2 = y[2 * e], hi2 = y[2 * e + 1];
-          x[2 * e] = lo * a.x - hi * a.y;
-          x[2 * e + 1] = lo * a.y + hi * a.x;
-          y[2 * e] = lo2 * b.x - hi2 * b.y;
-          y[2 * e + 1] = lo2 * b.y + hi2 * b.x;
-        }
-      } else {
+      for (int e = 0; e < 8; ++e) x[e] = fx[e], y[e] = fy[e];
+      if (turns) {
+        const double2* cs = turn + r * half + 8 * u;
+        if (A.neighbours) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const double2 a = cs[8 * u + e];
-          const double lo = x[e], hi = y[e];
-          x[e] = lo * a.x - hi * a.y;
-          y[e] = lo * a.y + hi * a.x;
+          for (int e = 0; e < 4; ++e) {
+            const double2 a = cs[e], b = cs[4 + e];
+            const double lo = x[2 * e], hi = x[2 * e + 1], lo2 = y[2 * e], hi2 = y[2 * e + 1];
+            x[2 * e] = lo * a.x - hi * a.y;
+            x[2 * e + 1] = lo * a.y + hi * a.x;
+            y[2 * e] = lo2 * b.x - hi2 * b.y;
+            y[2 * e + 1] = lo2 * b.y + hi2 * b.x;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const double2 a = cs[e];
+            const double lo = x[e], hi = y[e];
+            x[e] = lo * a.x - hi * a.y;
+            y[e] = lo * a.y + hi * a.x;
+          }
         }
       }
     }
-    if constexpr (KV == kPagedMxfp4) {  // a block is four chunks, of several threads
-      __syncthreads();
-      tops[slot][c0] = top_exponent(x);
-      tops[slot][c1] = top_exponent(y);
-      __syncthreads();
-    }
-    if (!on) continue;
     if (is_q) {
-      if (A.q) {
-        uint16_t* dst = A.q_out + (((size_t)i * A.h + head) * A.n + token) * D;
-        *reinterpret_cast<u32x4*>(dst + 8 * c0) = to_bf16(x);
-        *reinterpret_cast<u32x4*>(dst + 8 * c1) = to_bf16(y);
-      }
+      uint16_t* dst = A.q_out + (((size_t)i * A.h + head) * A.n + token) * D;
+      *reinterpret_cast<u32x4*>(dst + 8 * c0) = to_bf16(x);
+      *reinterpret_cast<u32x4*>(dst + 8 * c1) = to_bf16(y);
       continue;
     }
     const int row = start + token;
@@ -206,23 +228,47 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParam
     const size_t at = ((size_t)((int64_t)id * A.g + gam) << A.pool.shift) + (row & mask);
     uint8_t* dst = (is_k ? A.pool.K : A.pool.V) + at * RB;
     if constexpr (KV == kPagedBf16) {
-      *reinterpret_cast<u32x4*>(dst + 16 * c0) = to_bf16(x);
-      *reinterpret_cast<u32x4*>(dst + 16 * c1) = to_bf16(y);
+      *reinterpret_cast<u32x4*>(dst + 16 * c0) = is_k ? to_bf16(x) : rx;
+      *reinterpret_cast<u32x4*>(dst + 16 * c1) = is_k ? to_bf16(y) : ry;
     } else if constexpr (KV == kPagedFp8) {
       const float* sc = is_k ? A.pool.k_scale : A.pool.v_scale;
       const float s = sc ? sc[gam] : 1.f;
       if (t == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(A.status, kStatusScale);
       const double inv = 1.0 / (double)s;
+      if (!is_k) {
+        float f[8];
+        widen8(rx, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = f[e];
+        widen8(ry, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = f[e];
+      }
       *reinterpret_cast<u32x2*>(dst + 8 * c0) = to_fp8(x, inv);
       *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(y, inv);
     } else {
-      uint8_t* exps = (is_k ? A.pool.K_exp : A.pool.V_exp) + at * EB;
+      // A block is four chunks, of several of the row's threads: their
+      // exponents meet in LDS. A row's threads are neighbours in one wave,
+      // whose LDS accesses execute in order.
+      volatile int* ts = tops[slot];
+      ts[c0] = is_k ? top_exponent(x) : top_exponent(rx);
+      ts[c1] = is_k ? top_exponent(y) : top_exponent(ry);
+      __builtin_amdgcn_wave_barrier();
       const int b0 = c0 / 4, b1 = c1 / 4;
-      const int* ts = tops[slot];
       const uint32_t s0 = scale_byte(max(max(ts[4 * b0], ts[4 * b0 + 1]), max(ts[4 * b0 + 2], ts[4 * b0 + 3])));
       const uint32_t s1 = scale_byte(max(max(ts[4 * b1], ts[4 * b1 + 1]), max(ts[4 * b1 + 2], ts[4 * b1 + 3])));
-      *reinterpret_cast<uint32_t*>(dst + 4 * c0) = to_mx4(x, s0);
-      *reinterpret_cast<uint32_t*>(dst + 4 * c1) = to_mx4(y, s1);
+      __builtin_amdgcn_wave_barrier();
+      float fx[8], fy[8];
+      if (is_k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fx[e] = odd_f32(x[e]), fy[e] = odd_f32(y[e]);
+      } else {
+        widen8(rx, fx);
+        widen8(ry, fy);
+      }
+      uint8_t* exps = (is_k ? A.pool.K_exp : A.pool.V_exp) + at * EB;
+      *reinterpret_cast<uint32_t*>(dst + 4 * c0) = to_mx4(fx, s0);
+      *reinterpret_cast<uint32_t*>(dst + 4 * c1) = to_mx4(fy, s1);
       if (c0 % 4 == 0) exps[b0] = (uint8_t)s0;
       if (c1 % 4 == 0) exps[b1] = (uint8_t)s1;
     }
