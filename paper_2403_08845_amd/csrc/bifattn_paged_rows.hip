@@ -22,35 +22,60 @@ __device__ __forceinline__ float odd_f32(double x) {
   return __uint_as_float(u | 1u);
 }
 
-// Four words of two bf16 from 8 values, each rounded once. Going through fp32
-// rounds twice only where the fp32 value lies exactly between two bf16 ones
-// (its low half is 0x8000): those, one in 65536, take the way over odd_f32.
-__device__ __forceinline__ u32x4 to_bf16(const double* x) {
-  float f[8];
-  uint32_t near = 0xffffu;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    f[e] = (float)x[e];
-    near = min(near, (__float_as_uint(f[e]) ^ 0x8000u) & 0xffffu);
-  }
-  if (near == 0) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = odd_f32(x[e]);
-  }
+__device__ __forceinline__ u32x4 to_bf16(const float* f) {
   u32x4 r;
 #pragma unroll
   for (int w = 0; w < 4; ++w) r[w] = pack_bf16(f[2 * w], f[2 * w + 1]);
   return r;
 }
 
-// Eight OCP E4M3 codes of x / scale, saturated at +-448 (NaN stays NaN).
-__device__ __forceinline__ u32x2 to_fp8(const double* x, double inv) {
+// cos and sin of an angle, each as a part of 16 significant bits and the rest
+// (about 40 bits together): ch, cl, sh, sl.
+typedef f32x4 Turn;
+__device__ __forceinline__ void two_parts(double v, float& hi, float& lo) {
+  hi = __uint_as_float(__float_as_uint((float)v) & 0xffffff00u);
+  lo = (float)(v - (double)hi);
+}
+// (x cos - y sin, x sin + y cos) of bf16 values. x * ch and y * sh have at most
+// 24 bits, so y * sh is exact and the fused product rounds the exact main part
+// once: the result is off by 2^-22 of itself, also where the terms cancel. The
+// rest of an infinite element has no meaning; it is kept finite (a finite
+// element's is below 2^113), so that the main part decides.
+__device__ __forceinline__ float finite_rest(float r) { return __builtin_amdgcn_fmed3f(r, -0x1p120f, 0x1p120f); }
+__device__ __forceinline__ void rotate(float& x, float& y, const Turn& a) {
+  const float p = __builtin_fmaf(x, a[0], -(y * a[2])) + finite_rest(__builtin_fmaf(x, a[1], -(y * a[3])));
+  y = __builtin_fmaf(x, a[2], y * a[0]) + finite_rest(__builtin_fmaf(x, a[3], y * a[1]));
+  x = p;
+}
+// The same in 64 bits, times f and rounded to odd, for codes: an element next
+// to a border between two codes falls on its side.
+__device__ __forceinline__ void rotate_odd(float& x, float& y, const Turn& a, double f) {
+  const double c = (double)a[0] + (double)a[1], s = (double)a[2] + (double)a[3];
+  const double u = x, v = y;
+  x = odd_f32((u * c - v * s) * f);
+  y = odd_f32((u * s + v * c) * f);
+}
+// Two chunks of 8 whose elements rotate with `turn`: with each other, or in
+// neighbouring pairs.
+template <typename F>
+__device__ __forceinline__ void rotate_chunks(float* x, float* y, const Turn* a, bool neighbours, F&& turn) {
+  if (neighbours) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      turn(x[2 * e], x[2 * e + 1], a[e]);
+      turn(y[2 * e], y[2 * e + 1], a[4 + e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) turn(x[e], y[e], a[e]);
+  }
+}
+
+// Eight OCP E4M3 codes, saturated at +-448 (NaN stays NaN).
+__device__ __forceinline__ u32x2 to_fp8(const float* x) {
   float f[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float y = odd_f32(x[e] * inv);
-    f[e] = y > 448.f ? 448.f : (y < -448.f ? -448.f : y);
-  }
+  for (int e = 0; e < 8; ++e) f[e] = x[e] > 448.f ? 448.f : (x[e] < -448.f ? -448.f : x[e]);
   u32x2 r;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
@@ -61,28 +86,17 @@ __device__ __forceinline__ u32x2 to_fp8(const double* x, double inv) {
   return r;
 }
 
-// Biased exponent (that of a 64-bit number) of the largest of 8 magnitudes:
-// 0x7ff when one is not finite. The high words alone order the exponents.
-__device__ __forceinline__ int top_exponent(const double* x) {
+// Biased exponent of the largest of 8 magnitudes, 255 when one is not finite.
+__device__ __forceinline__ int top_exponent(const float* f) {
   uint32_t t = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) t = max(t, (uint32_t)__double2hiint(x[e]) & 0x7fffffffu);
-  return (int)(t >> 20);
-}
-// The same of 8 bf16 values as they are stored.
-__device__ __forceinline__ int top_exponent(const u32x4& r) {
-  uint32_t t = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) t = max(t, max(r[w] & 0x7fffu, (r[w] >> 16) & 0x7fffu));
-  const int e = (int)(t >> 7);
-  return e == 255 ? 0x7ff : e + (t ? 1023 - 127 : 0);  // (bf16 subnormals: below any scale's range)
+  for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(f[e]) & 0x7fffffffu);
+  return (int)(t >> 23);
 }
 // Scale byte of a block whose largest magnitude has that exponent: 2^(byte -
 // 127) with byte - 127 = floor(log2(largest)) - 2 within [-126, 127] (the
 // largest E2M1 value is 1.5 * 2^2), 255 for a block that is not finite.
-__device__ __forceinline__ uint32_t scale_byte(int top) {
-  return top == 0x7ff ? 255u : (uint32_t)min(254, max(1, top - 1023 - 2 + 127));
-}
+__device__ __forceinline__ uint32_t scale_byte(int top) { return top == 255 ? 255u : (uint32_t)max(1, top - 2); }
 // Eight E2M1 codes of f 2^(127 - byte), to nearest even, saturated at 6.
 __device__ __forceinline__ uint32_t to_mx4(const float* f, uint32_t byte) {
   const float s = __uint_as_float(byte << 23);
@@ -100,25 +114,26 @@ __device__ __forceinline__ void widen8(const u32x4& r, float* f) {
     f[2 * w + 1] = __uint_as_float(r[w] & 0xffff0000u);
   }
 }
+
 // Append. Work-group: sample i, tokens_per_block tokens, heads_per_block of the
 // h query rows, g key rows and g value rows of each. A row is d/16 threads'
 // work, each two chunks of 8 elements that rotate with each other.
 //
 // The angle of a pair is position * freq in 64 bits (positions reach 2^31 and
 // an fp32 product is off by 2^-24 of a turn per turn: 0.06 of a radian at 10^6),
-// formed once per token and pair and kept in LDS; the rotation is exact to 64
-// bits and each element is rounded once, to its stored type, so that codes next
-// to a border fall on the right side.
+// formed once per token and pair and kept in LDS. Rotated queries and bf16 keys
+// are off by 2^-22 of themselves before their one rounding, codes are formed
+// from 64 bits.
 //
 // Byte work where the batch is large; a step of some tokens is one launch's
 // latency (a chain of loads: length, table entry, row).
 template <int D, int KV>
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParams A) {
+__global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(4))) void append_kernel(PagedAppendParams A) {
   constexpr int TPR = D / 16;                       // threads of a row
   constexpr int ROWS = kAppendThreads / TPR;        // rows in flight
   constexpr int RB = paged_row_bytes(D, KV), EB = D / kMxBlock;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
-  double2* turn = reinterpret_cast<double2*>(dyn);  // [tokens_per_block][rot/2]: cos, sin
+  Turn* turn = reinterpret_cast<Turn*>(dyn);  // [tokens_per_block][rot/2]
   __shared__ int tops[ROWS][D / 8];
   const int per = A.token_blocks * A.head_blocks;
   const int i = blockIdx.x / per, in = blockIdx.x - i * per;
@@ -137,7 +152,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParam
     const double rev = (double)((int64_t)A.position0 + start + t0 + t) * ((double)A.freqs[j] * 0.15915494309189533577);
     double s, c;
     sincospi(2.0 * (rev - rint(rev)), &s, &c);
-    turn[k] = double2{c, s};
+    float ch, cl, sh, sl;
+    two_parts(c, ch, cl);
+    two_parts(s, sh, sl);
+    turn[k] = Turn{ch, cl, sh, sl};
   }
   __syncthreads();  // also: every thread has read lens
   if (threadIdx.x == 0) {
@@ -161,61 +179,26 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParam
   const int rc = A.rot / 16;  // threads with rotated chunks
   const bool turns = u < rc;
   const int c0 = base + (turns && !A.neighbours ? u : 2 * u), c1 = turns && !A.neighbours ? c0 + rc : c0 + 1;
-  // The next row's chunks are requested before this row's are worked on.
-  auto fetch = [&](int item, u32x4& rx, u32x4& ry) {
-    const int it = min(item, items - 1), r = it / nh, head = h0 + it - r * nh;
-    const bool is_q = head < A.h, is_k = !is_q && head < A.h + A.g;
-    const int64_t* st = is_q ? A.qs : (is_k ? A.ks : A.vs);
-    const uint16_t* src = (is_q ? A.q : (is_k ? A.k : A.v)) + (int64_t)i * st[0] +
-                          (is_q ? head : (is_k ? head - A.h : head - A.h - A.g)) * st[1] + (t0 + r) * st[2];
-    rx = load16(src + 8 * c0);
-    ry = load16(src + 8 * c1);
-  };
-  if (items == 0) return;
-  u32x4 nx, ny;
-  fetch(slot, nx, ny);
-  for (int first = 0; first < items; first += ROWS) {
-    const int item = first + slot;
-    const u32x4 rx = nx, ry = ny;
-    if (first + ROWS < items) fetch(item + ROWS, nx, ny);
-    if (item >= items) continue;
-    const int r = item / nh, head = h0 + item - r * nh, token = t0 + r;
+  // Row `slot` of every pass: r-th token, head h0 + hd (kept without divisions).
+  int r = slot / nh, hd = slot % nh;
+  const int dr = ROWS / nh, dh = ROWS % nh;
+  for (int item = slot; item < items; item += ROWS, r += dr, hd += dh) {
+    if (hd >= nh) hd -= nh, ++r;
+    const int head = h0 + hd, token = t0 + r;
     const bool is_q = head < A.h, is_k = !is_q && head < A.h + A.g;
     const int gam = is_q ? 0 : (is_k ? head - A.h : head - A.h - A.g);
-    double x[8], y[8];
-    if (is_q || is_k) {
-      float fx[8], fy[8];
-      widen8(rx, fx);
-      widen8(ry, fy);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = fx[e], y[e] = fy[e];
-      if (turns) {
-        const double2* cs = turn + r * half + 8 * u;
-        if (A.neighbours) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const double2 a = cs[e], b = cs[4 + e];
-            const double lo = x[2 * e], hi = x[2 * e + 1], lo2 = y[2 * e], hi2 = y[2 * e + 1];
-            x[2 * e] = lo * a.x - hi * a.y;
-            x[2 * e + 1] = lo * a.y + hi * a.x;
-            y[2 * e] = lo2 * b.x - hi2 * b.y;
-            y[2 * e + 1] = lo2 * b.y + hi2 * b.x;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const double2 a = cs[e];
-            const double lo = x[e], hi = y[e];
-            x[e] = lo * a.x - hi * a.y;
-            y[e] = lo * a.y + hi * a.x;
-          }
-        }
-      }
-    }
+    const int64_t* st = is_q ? A.qs : (is_k ? A.ks : A.vs);
+    const uint16_t* src = (is_q ? A.q : (is_k ? A.k : A.v)) + (int64_t)i * st[0] + (is_q ? head : gam) * st[1] + token * st[2];
+    const u32x4 rx = load16(src + 8 * c0), ry = load16(src + 8 * c1);
+    const Turn* angles = turn + r * half + 8 * u;
+    float fx[8], fy[8];
+    widen8(rx, fx);
+    widen8(ry, fy);
     if (is_q) {
+      if (turns) rotate_chunks(fx, fy, angles, A.neighbours, rotate);
       uint16_t* dst = A.q_out + (((size_t)i * A.h + head) * A.n + token) * D;
-      *reinterpret_cast<u32x4*>(dst + 8 * c0) = to_bf16(x);
-      *reinterpret_cast<u32x4*>(dst + 8 * c1) = to_bf16(y);
+      *reinterpret_cast<u32x4*>(dst + 8 * c0) = to_bf16(fx);
+      *reinterpret_cast<u32x4*>(dst + 8 * c1) = to_bf16(fy);
       continue;
     }
     const int row = start + token;
@@ -227,45 +210,38 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedAppendParam
     }
     const size_t at = ((size_t)((int64_t)id * A.g + gam) << A.pool.shift) + (row & mask);
     uint8_t* dst = (is_k ? A.pool.K : A.pool.V) + at * RB;
+    const bool rotates = is_k && turns;
     if constexpr (KV == kPagedBf16) {
-      *reinterpret_cast<u32x4*>(dst + 16 * c0) = is_k ? to_bf16(x) : rx;
-      *reinterpret_cast<u32x4*>(dst + 16 * c1) = is_k ? to_bf16(y) : ry;
+      if (rotates) rotate_chunks(fx, fy, angles, A.neighbours, rotate);
+      *reinterpret_cast<u32x4*>(dst + 16 * c0) = to_bf16(fx);
+      *reinterpret_cast<u32x4*>(dst + 16 * c1) = to_bf16(fy);
     } else if constexpr (KV == kPagedFp8) {
       const float* sc = is_k ? A.pool.k_scale : A.pool.v_scale;
       const float s = sc ? sc[gam] : 1.f;
       if (t == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(A.status, kStatusScale);
       const double inv = 1.0 / (double)s;
-      if (!is_k) {
-        float f[8];
-        widen8(rx, f);
+      if (rotates) {
+        rotate_chunks(fx, fy, angles, A.neighbours, [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, inv); });
+      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = f[e];
-        widen8(ry, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = f[e];
+        for (int e = 0; e < 8; ++e) fx[e] = odd_f32(fx[e] * inv), fy[e] = odd_f32(fy[e] * inv);
       }
-      *reinterpret_cast<u32x2*>(dst + 8 * c0) = to_fp8(x, inv);
-      *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(y, inv);
+      *reinterpret_cast<u32x2*>(dst + 8 * c0) = to_fp8(fx);
+      *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(fy);
     } else {
+      if (rotates)
+        rotate_chunks(fx, fy, angles, A.neighbours, [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, 1.0); });
       // A block is four chunks, of several of the row's threads: their
       // exponents meet in LDS. A row's threads are neighbours in one wave,
       // whose LDS accesses execute in order.
       volatile int* ts = tops[slot];
-      ts[c0] = is_k ? top_exponent(x) : top_exponent(rx);
-      ts[c1] = is_k ? top_exponent(y) : top_exponent(ry);
+      ts[c0] = top_exponent(fx);
+      ts[c1] = top_exponent(fy);
       __builtin_amdgcn_wave_barrier();
       const int b0 = c0 / 4, b1 = c1 / 4;
       const uint32_t s0 = scale_byte(max(max(ts[4 * b0], ts[4 * b0 + 1]), max(ts[4 * b0 + 2], ts[4 * b0 + 3])));
       const uint32_t s1 = scale_byte(max(max(ts[4 * b1], ts[4 * b1 + 1]), max(ts[4 * b1 + 2], ts[4 * b1 + 3])));
       __builtin_amdgcn_wave_barrier();
-      float fx[8], fy[8];
-      if (is_k) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) fx[e] = odd_f32(x[e]), fy[e] = odd_f32(y[e]);
-      } else {
-        widen8(rx, fx);
-        widen8(ry, fy);
-      }
       uint8_t* exps = (is_k ? A.pool.K_exp : A.pool.V_exp) + at * EB;
       *reinterpret_cast<uint32_t*>(dst + 4 * c0) = to_mx4(fx, s0);
       *reinterpret_cast<uint32_t*>(dst + 4 * c1) = to_mx4(fy, s1);
@@ -343,7 +319,7 @@ hipError_t go(void (*kernel)(Prm), int grid, int block, int lds, hipStream_t str
 
 hipError_t launch_paged_append(const PagedAppendParams& A, int kv, hipStream_t s, hipEvent_t stop) {
   const int grid = A.samples * A.token_blocks * A.head_blocks;
-  const int lds = A.tokens_per_block * (A.rot / 2) * (int)sizeof(double2);
+  const int lds = A.tokens_per_block * (A.rot / 2) * (int)sizeof(Turn);
   auto run = [&](auto kernel) { return go(kernel, grid, kAppendThreads, lds, s, stop, A); };
   if (A.d == 128) {
     if (kv == kPagedBf16) return run(append_kernel<128, kPagedBf16>);

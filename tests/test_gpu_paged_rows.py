@@ -319,3 +319,25 @@ def test_streams_other_than_the_current_one():
             assert bif.bifattn_paged_plan_status(plan, stream) == bif.OK
         res.append((pages.K, q_out, lens))
     assert all(torch.equal(a.contiguous().view(torch.uint8), z.contiguous().view(torch.uint8)) for a, z in zip(*res))
+
+
+def test_rotation_of_infinite_elements():
+    """An infinite element makes its pair infinite (the sign of its cosine and
+    sine) and leaves the others alone."""
+    x = Problem(1, 1, 1, 64, 0, 1, page=16, lens=[1], seed=9)
+    row = torch.randn(64, generator=x.rng)
+    row[3], row[40] = float("inf"), float("-inf")
+    kv = row.to(torch.bfloat16).view(1, 1, 1, 64).cuda()
+    f = torch.linspace(0.1, 1.4, 32)
+    pages = x.pages()
+    lens = torch.zeros(1, dtype=torch.int32, device="cuda")
+    x.m_c = 1  # position 1: angles in the first quadrant
+    out = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    with x.plan() as plan:
+        bif.bifattn_paged_append(plan, pages, x.tables.cuda(), lens, kv, kv, lens, q=kv, q_out=out, freqs=f.cuda())
+        assert bif.bifattn_paged_plan_status(plan) == bif.OK
+    for got in (out[0, 0, 0].cpu(), pages.K[int(x.tables[0, 0]), 0, 0].cpu()):
+        inf = torch.zeros(64)
+        inf[3], inf[35], inf[40], inf[8] = 1, 1, -1, 1  # (x c - y s, x s + y c)
+        assert torch.equal(torch.isinf(got.float()) * torch.sign(got.float()), inf)
+        assert not torch.isnan(got).any()
