@@ -748,18 +748,35 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
     const unsigned char* kb = lds + buf * STAGE + kbase;
     const unsigned char* vb = lds + buf * STAGE + vbase;
     const int rem = nkeys - st * SK;
+    // LDS reads ahead of their use: a block's V^T operands are read while its
+    // weights are formed, the next block's K operands during the value products.
+    u32x4 kw[KSTEPS];
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) kw[ks] = read128(kb + 32 * ks);
 #pragma unroll
     for (int b = 0; b < SK / 32; ++b) {
       f32x16 sacc;
 #pragma unroll
       for (int v = 0; v < 16; ++v) sacc[v] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks) sacc = mfma32(read128(kb + 32 * b * KROW + 32 * ks), qop[ks], sacc);
+      for (int ks = 0; ks < KSTEPS; ++ks) sacc = mfma32(kw[ks], qop[ks], sacc);
+      __builtin_amdgcn_sched_barrier(0);
+      u32x4 vw[2][DB];
+#pragma unroll
+      for (int ss = 0; ss < 2; ++ss)
+#pragma unroll
+        for (int t = 0; t < DB; ++t) {
+          const unsigned char* p = vb + (32 * b + 16 * ss) * VROW + 64 * t;
+          const u32x2 v0 = read_tr(p), v1 = read_tr(p + 8 * VROW);
+          vw[ss][t] = u32x4{v0[0], v0[1], v1[0], v1[1]};
+        }
+      __builtin_amdgcn_sched_barrier(0);
       float x[16];
 #pragma unroll
       for (int v = 0; v < 16; ++v) x[v] = sacc[v];
       if (rem < 32 * (b + 1)) {
-        const int nv = __builtin_amdgcn_readfirstlane(rem) - 32 * b;
+        asm volatile("");  // a branch: 32 selects in every block otherwise
+        const int nv = rem - 32 * b;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (8 * (v / 4) + 4 * h + (v & 3) >= nv) x[v] = kNegInf;
@@ -794,28 +811,31 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
       lsum += ps;
       // O^T += V^T P^T: k-step ss holds the lane's elements 8ss..8ss+7, keys
       // 16ss + 8(e/4) + 4h + e%4, the keys that the transposing reads deliver.
+      u32x4 hi[2], lo[2];
 #pragma unroll
       for (int ss = 0; ss < 2; ++ss) {
-        uint32_t hi[4], lo[4];
+        uint32_t h4[4], l4[4] = {0, 0, 0, 0};
         if constexpr (kHalf) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w) hi[w] = pack_f16(pr[8 * ss + 2 * w], pr[8 * ss + 2 * w + 1]);
+          for (int w = 0; w < 4; ++w) h4[w] = pack_f16(pr[8 * ss + 2 * w], pr[8 * ss + 2 * w + 1]);
         } else {
-          split_weights<4>(pr + 8 * ss, hi, lo);
+          split_weights<4>(pr + 8 * ss, h4, l4);
         }
+        hi[ss] = u32x4{h4[0], h4[1], h4[2], h4[3]};
+        lo[ss] = u32x4{l4[0], l4[1], l4[2], l4[3]};
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (b + 1 < SK / 32)
 #pragma unroll
-        for (int t = 0; t < DB; ++t) {
-          const unsigned char* p = vb + (32 * b + 16 * ss) * VROW + 64 * t;
-          const u32x2 v0 = read_tr(p), v1 = read_tr(p + 8 * VROW);
-          const u32x4 v = u32x4{v0[0], v0[1], v1[0], v1[1]};
-          const u32x4 first = u32x4{hi[0], hi[1], hi[2], hi[3]};
-          if constexpr (kHalf) {
-            acc[t] = mfma32_f16(v, first, acc[t]);
-          } else {
-            acc[t] = mfma32(v, first, acc[t]);
-            acc[t] = mfma32(v, u32x4{lo[0], lo[1], lo[2], lo[3]}, acc[t]);
-          }
-        }
+        for (int ks = 0; ks < KSTEPS; ++ks) kw[ks] = read128(kb + 32 * (b + 1) * KROW + 32 * ks);
+#pragma unroll
+      for (int ss = 0; ss < 2; ++ss) {
+#pragma unroll
+        for (int t = 0; t < DB; ++t)
+          acc[t] = kHalf ? mfma32_f16(vw[ss][t], hi[ss], acc[t]) : mfma32(vw[ss][t], hi[ss], acc[t]);
+        if constexpr (!kHalf)
+#pragma unroll
+          for (int t = 0; t < DB; ++t) acc[t] = mfma32(vw[ss][t], lo[ss], acc[t]);
       }
     }
   }
