@@ -104,6 +104,65 @@ int own_chunk(int64_t units, int64_t rows) {
   return keys;
 }
 
+// Waves per work-group (8 or 4) and key splits of a many-row context part: the
+// least of an estimate of the step's time over both and over the splits. Its
+// terms are the parts of a step (a context work-group's start and keys, the
+// own-row work-groups beside the last round of context ones, the partials and
+// the combine's loads), its constants a fit of whole steps: 1500 random layers
+// (33 to 10^4 rows per group, 0.1k to 40k keys, every type, both head kinds) at
+// about ten settings each. Over 1500 others the choice is 1.6% slower than the
+// best of those settings on average, 8% at the 95th percentile, 22% at worst; a fixed number
+// of work-groups (160 of eight waves, 256 of four) 12%, 37% and up to 2.8 times.
+struct ManySplit {
+  int waves = 4;
+  int64_t splits = 1;
+};
+int many_step(int waves) { return waves == 8 ? 128 : 64; }  // keys of a stage
+ManySplit many_row_split(const bifattn_paged_plan_s* P) {
+  const bifattn_paged_dims_t& d = P->dims;
+  const bool half = d.d == 64;
+  const int64_t units = (int64_t)d.b * d.g;
+  const int64_t own = P->dec_tiles <= 2 ? units * P->S_d : 0;  // own-row work-groups in the launch
+  const double codes = d.kv_type == BIFATTN_KV_BF16 ? 1.0 : d.kv_type == BIFATTN_KV_FP8_E4M3 ? 0.6 : 0.4;
+  const double bytes = 2.0 * d.g * paged_row_bytes(d.d, d.kv_type) * ((double)d.m_c + 0.75 * (double)d.b * d.m_d_max);
+  const double kv = d.kv_type == BIFATTN_KV_BF16 ? 1.41 : d.kv_type == BIFATTN_KV_FP8_E4M3 ? 0.84 : 1.08;
+  const double td = 2.93 + 1.69 * (half ? 0.5 : 1.0) * codes * std::min(P->dec_keys, d.m_d_max) / 128.0;
+  ManySplit best;
+  double least = -1.0;
+  for (int waves = 4; waves <= 8; waves += 4) {
+    const int64_t slots = waves == 8 ? kCUs : (half ? 3 : 2) * kCUs;
+    const int64_t per_split = (int64_t)d.g * P->maps * ceil_div(P->Mh, 32 * waves);
+    const int64_t own_wgs = ceil_div(own, waves / kWaves);
+    const int64_t most = std::max<int64_t>(1, std::min(ceil_div(d.m_c, many_step(waves)), 4 * kCUs / per_split));
+    for (int64_t S = 1; S <= most; S += 1 + S / 8) {
+      const int64_t keys = round_up(ceil_div(d.m_c, S), many_step(waves));
+      const int64_t parts = ceil_div(d.m_c, keys), wgs = per_split * parts;
+      // the clock gives way as more than five eighths of the CUs run context
+      // work-groups; those that share a CU slow each other
+      const double busy = (1.0 + 0.06 * (double)std::max<int64_t>(0, std::min<int64_t>(wgs, kCUs) - 160) / 96.0) *
+                          (1.0 + 0.38 * (double)(ceil_div(std::min(wgs, slots), kCUs) - 1));
+      const double tc = (waves == 8 ? 4.5 : 3.0) + (waves == 8 ? 0.0198 : 0.0194) * (half ? 0.58 : 1.0) *
+                                                       (P->maps == 2 ? 0.89 : 1.0) * kv * (double)keys * busy;
+      const int64_t rem = wgs % slots;
+      const double tr = rem ? tc : 0.0, alone = (double)ceil_div(own_wgs, slots - rem) * td;
+      const double beside = own_wgs == 0       ? 0.0
+                            : alone <= tr + td ? alone
+                                               : ((double)rem * tc + (double)own_wgs * td) / (double)slots + 0.23 * td;
+      double t = (double)(wgs / slots) * tc + std::max(tr, beside) + 0.05 * std::min(tr, beside);
+      t = std::max(t, bytes / 7.5e6);
+      const int64_t loads = ceil_div(parts * d.d, 256) + ceil_div(4 * (int64_t)P->S_d * d.d, 256);
+      t += 1.66 * P->maps * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3072 ? 8 : 16) - 1) +
+           (double)(parts + 4 * P->S_d) * P->M * d.g * (d.d * 4 + 16) / 2.1e6;
+      if (least < 0.0 || t < least) {
+        least = t;
+        best.waves = waves;
+        best.splits = S;
+      }
+    }
+  }
+  return best;
+}
+
 bifattn_status_t split_work(bifattn_paged_plan_s* P) {
   const bifattn_paged_dims_t& d = P->dims;
   P->ntok = d.n > 0 ? d.n : 1;
@@ -137,14 +196,15 @@ bifattn_status_t split_work(bifattn_paged_plan_s* P) {
     P->S_c = (int)ceil_div(d.m_c, P->ctx_keys);
     P->n_ctx_small_blocks = d.g * P->S_c;
   } else {
-    P->ctx_wide = P->Mh >= 256 ? 8 : 4;
-    P->ctx_wide = env_int("BIFATTN_CTX_WIDE", P->ctx_wide) == 8 ? 8 : 4;
+    ManySplit split = many_row_split(P);
+    const int wgs = env_int("BIFATTN_CTX_WGS", 0);
+    if (wgs > 0) {
+      split.waves = env_int("BIFATTN_CTX_WIDE", split.waves) == 8 ? 8 : 4;
+      split.splits = ceil_div(wgs, (int64_t)d.g * P->maps * ceil_div(P->Mh, 32 * split.waves));
+    }
+    P->ctx_wide = split.waves;
     P->ctx_row_blocks = P->maps * (int)ceil_div(P->Mh, 32 * P->ctx_wide);
-    const int step = P->ctx_wide == 8 ? 128 : 64;
-    const int target = env_int("BIFATTN_CTX_WGS", P->ctx_wide == 8 ? (P->n_dec_blocks ? 160 : kCUs)
-                                                                  : (P->n_dec_blocks ? kCUs : 2 * kCUs));
-    const int64_t splits = std::max<int64_t>(1, ceil_div(target, (int64_t)d.g * P->ctx_row_blocks));
-    P->ctx_keys = (int)round_up(ceil_div(d.m_c, splits), step);
+    P->ctx_keys = (int)round_up(ceil_div(d.m_c, split.splits), many_step(P->ctx_wide));
     P->S_c = (int)ceil_div(d.m_c, P->ctx_keys);
     if ((int64_t)d.g * P->S_c * P->ctx_row_blocks > INT32_MAX / 4) return BIFATTN_EINVAL;
     P->n_ctx_blocks = d.g * P->S_c * P->ctx_row_blocks;
