@@ -388,7 +388,8 @@ bifattn_status_t bifattn_paged_plan_create(const bifattn_paged_dims_t *dims,
                                            bifattn_paged_plan_t *plan);
 /* As bifattn_plan_destroy. */
 bifattn_status_t bifattn_paged_plan_destroy(bifattn_paged_plan_t plan);
-/* As bifattn_plan_get_info (path is always BIFATTN_PATH_BIFURCATED). */
+/* As bifattn_plan_get_info. path is BIFATTN_PATH_STANDARD where an attention step is one launch
+ * without partials, which an estimate picks for small steps; the splits are then not used. */
 bifattn_status_t bifattn_paged_plan_get_info(bifattn_paged_plan_t plan, bifattn_plan_info_t *info);
 /* Synchronise `stream`, then report and clear the plan's device-side flags:
  * BIFATTN_EPAGE, else BIFATTN_ESCALE, else BIFATTN_ELENS (a length or count

@@ -79,6 +79,12 @@ struct PagedCombineParams {
   int S_c, S_d;          // context splits, decode partials (4 per chunk)
 };
 
+// Small steps: both parts and the end of the row in one kernel.
+struct PagedWholeParams {
+  PagedAttnParams A;
+  PagedCombineParams C;
+};
+
 struct PagedAppendParams {
   PagePool pool;
   const int32_t* table;     // [samples][table_pages]
@@ -120,6 +126,9 @@ hipError_t launch_paged_stream(const PagedAttnParams& P, int d, int kv, int ctx_
 // Many-row launch: n_ctx_blocks context work-groups, then n_dec_blocks decode
 // ones (dec_tiles at most 2).
 hipError_t launch_paged_wide(const PagedAttnParams& P, int d, int kv, int dec_tiles, hipStream_t stream);
+// Small steps: one work-group per (sample, group), `tiles` (1 or 2) query tiles.
+hipError_t launch_paged_whole(const PagedWholeParams& W, int d, int kv, int tiles, hipStream_t stream,
+                              hipEvent_t stop);
 hipError_t launch_paged_combine(const PagedCombineParams& C, int d, hipStream_t stream, hipEvent_t stop);
 hipError_t launch_paged_append(const PagedAppendParams& A, int kv, hipStream_t stream, hipEvent_t stop);
 hipError_t launch_paged_gather(const PagedGatherParams& G, int kv, hipStream_t stream, hipEvent_t stop);

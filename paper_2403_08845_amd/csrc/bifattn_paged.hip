@@ -96,8 +96,8 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ f32x16 mfma32_f16(const u32x4& a, const u32x4& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ uint32_t load_u8(__amdgpu_buffer_rsrc_t r, int off) {
-  return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, off, 0, kAuxStream);
+template <int AUX> __device__ __forceinline__ uint32_t load_u8(__amdgpu_buffer_rsrc_t r, int off) {
+  return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, off, 0, AUX);
 }
 
 // Padded rows in LDS: 16 key rows of an operand read start in different
@@ -132,6 +132,8 @@ template <int D, typename KV> struct PageTile {
   typename L::type k[2][HI], v[2][HI];
   uint32_t ke[2], ve[2];
 
+  // AUX: cache policy (rows that are read once stream past the caches).
+  template <int AUX>
   __device__ __forceinline__ void load(const PagePool& P, int gam, int id0, int id1, int key0, int k1,
                                        int lane) {
 #pragma unroll
@@ -144,14 +146,14 @@ template <int D, typename KV> struct PageTile {
 #pragma unroll
       for (int e = 0; e < HI; ++e) {
         const int at = KV::MX ? (lane & 15) * RB + (lane >> 4) * LB : (64 * e + lane) * LB;
-        k[a][e] = L::template load<kAuxStream>(rk, at);
-        v[a][e] = L::template load<kAuxStream>(rv, (64 * e + lane) * LB);
+        k[a][e] = L::template load<AUX>(rk, at);
+        v[a][e] = L::template load<AUX>(rv, (64 * e + lane) * LB);
       }
       if constexpr (KV::MX) {
         const __amdgpu_buffer_rsrc_t re = half_rsrc(P.K_exp + row * EB, n, EB);
         const __amdgpu_buffer_rsrc_t rf = half_rsrc(P.V_exp + row * EB, n, EB);
-        ke[a] = load_u8(re, (lane & 15) * EB + ((lane >> 4) * EB) / 4);
-        ve[a] = load_u8(rf, (lane * EB) / 4);
+        ke[a] = load_u8<AUX>(re, (lane & 15) * EB + ((lane >> 4) * EB) / 4);
+        ve[a] = load_u8<AUX>(rf, (lane * EB) / 4);
       }
     }
   }
@@ -351,7 +353,7 @@ __device__ __forceinline__ int tile_ids(const int32_t* table, int key, int end, 
 // requested an iteration before its rows, ahead of rows that are waited for
 // anyway. kend: the end that the tokens' limits count from. Returns whether a
 // page id was outside the pool (read as page 0).
-template <int D, int NT, typename KV, typename QAt>
+template <int D, int NT, typename KV, int AUX = kAuxStream, typename QAt>
 __device__ __forceinline__ bool stream_pages(PageState<D, NT>& st, const PagePool& P, int gam,
                                              const int32_t* table, QAt&& q_at, unsigned char* kl,
                                              unsigned char* vl, int ids0, int ids1, int k0, int k1, int kend,
@@ -364,7 +366,7 @@ __device__ __forceinline__ bool stream_pages(PageState<D, NT>& st, const PagePoo
     const bool wrong = (unsigned)ids >= (unsigned)P.num_pages;
     bad |= wrong && key + 16 * (lane & 1) < k1;
     ids = wrong ? 0 : ids;
-    t.load(P, gam, __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), min(key, k1), k1, lane);
+    t.template load<AUX>(P, gam, __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), min(key, k1), k1, lane);
   };
   auto ids_at = [&](int key) { return tile_ids(table, min(key, k1 - 1), k1, P.shift, lane); };
   load(T[0], ids0, k0);
@@ -471,6 +473,39 @@ template <int D, int NT> struct PageMerge {
   static constexpr int bytes = (ROWS * LD + 2 * ROWS) * 4;
 };
 
+// Merge the four waves' states of the same rows in LDS, in wave order: row r is
+// then merge[r*LD ..], its maximum and sum behind the rows.
+template <int D, int NT>
+__device__ __forceinline__ void merge_states(const PageState<D, NT>& st, float* merge, int wave, int lane) {
+  constexpr int LD = PageMerge<D, NT>::LD, ROWS = PageMerge<D, NT>::ROWS;
+  float* m_s = merge + ROWS * LD;
+  float* l_s = m_s + ROWS;
+  const int n = lane & 15, G = lane >> 4;
+  __syncthreads();  // the merge buffer overlays the waves' tiles
+  for (int turn = 0; turn < kWaves; ++turn) {
+    if (wave == turn) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = nt * kRowsPerTile + n;
+        const float mo = turn ? m_s[row] : kNegInf, lo = turn ? l_s[row] : 0.f;
+        const float mn = fmaxf(mo, st.mref[nt]), base = mn == kNegInf ? 0.f : mn;
+        const float fa = exp2_fast(mo - base), fb = exp2_fast(st.mref[nt] - base);
+        float* dst = merge + row * LD + 4 * G;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+          const f32x4 old = turn ? *reinterpret_cast<f32x4*>(dst + 16 * t) : f32x4{0.f, 0.f, 0.f, 0.f};
+          *reinterpret_cast<f32x4*>(dst + 16 * t) = old * fa + st.acc[nt][t] * fb;
+        }
+        if (G == 0) {
+          m_s[row] = mn;
+          l_s[row] = lo * fa + st.l[nt] * fb;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
 struct GroupRows {  // row u*Mh + i*pn + jp of a group
   const uint16_t* base;
   int D, M, Mh, pn, hn;
@@ -514,32 +549,9 @@ __device__ __forceinline__ void ctx_few_block(const PagedAttnParams& P, int blk,
                                            1, group_scale_log2(P, gam), lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
-  float* m_s = merge + ROWS * LD;
-  float* l_s = m_s + ROWS;
-  const int n = lane & 15, G = lane >> 4;
-  __syncthreads();  // the merge buffer overlays the waves' tiles
-  for (int turn = 0; turn < kWaves; ++turn) {
-    if (wave == turn) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int row = nt * kRowsPerTile + n;
-        const float mo = turn ? m_s[row] : kNegInf, lo = turn ? l_s[row] : 0.f;
-        const float mn = fmaxf(mo, st.mref[nt]), base = mn == kNegInf ? 0.f : mn;
-        const float fa = exp2_fast(mo - base), fb = exp2_fast(st.mref[nt] - base);
-        float* dst = merge + row * LD + 4 * G;
-#pragma unroll
-        for (int t = 0; t < D / 16; ++t) {
-          const f32x4 old = turn ? *reinterpret_cast<f32x4*>(dst + 16 * t) : f32x4{0.f, 0.f, 0.f, 0.f};
-          *reinterpret_cast<f32x4*>(dst + 16 * t) = old * fa + st.acc[nt][t] * fb;
-        }
-        if (G == 0) {
-          m_s[row] = mn;
-          l_s[row] = lo * fa + st.l[nt] * fb;
-        }
-      }
-    }
-    __syncthreads();
-  }
+  merge_states(st, merge, wave, lane);
+  const float* m_s = merge + ROWS * LD;
+  const float* l_s = m_s + ROWS;
   const size_t prow = (size_t)blk * M;
   for (int idx = threadIdx.x; idx < M * (D / 4); idx += kThreads) {
     const int row = idx / (D / 4), c = idx % (D / 4);
@@ -882,6 +894,26 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
   own_block<D, NTD, KV>(P, blk, blk < P.n_dec_blocks, wave % kWaves, lane, lds + unit * QB, kl, kl + S::KT);
 }
 
+// The end of a row's work: the maps' difference, the head's norm and the one
+// rounding. Row j of a sample (head x token), elements col .. col + 3 of each map in
+// the d/4 lanes of the row; the packed elements of this lane.
+template <int D, int MAPS>
+__device__ __forceinline__ u32x2 finish_row(const PagedCombineParams& C, int j, const f32x4& y0, const f32x4& y1, int col) {
+  f32x4 r = y0;
+  if constexpr (MAPS == 2) {
+    r -= C.lambda[j / C.ntok] * y1;
+    if (C.weight) {
+      float sq = r[0] * r[0] + r[1] * r[1] + r[2] * r[2] + r[3] * r[3];
+      if constexpr (D == 128) sq = xor16_sum(sq);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
+      r *= *reinterpret_cast<const f32x4*>(C.weight + col) / sqrtf(sq * (1.f / D) + C.eps);
+    }
+    r *= C.out_scale;
+  }
+  return u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+}
+
 // ---------------------------------------------------------------------------
 // Combine: a wave per output row merges the row's partials (of each map) into
 //   softmax @ V = vs sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k
@@ -908,9 +940,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedCombineParams C
     if (!ok) atomicOr(C.status, kStatusScale);
   }
   const int np = C.S_c + C.S_d;
-  f32x4 y[MAPS];
-#pragma unroll
-  for (int map = 0; map < MAPS; ++map) {
+  auto merged = [&](int map) {
     const size_t cbase = (size_t)gam * C.S_c * C.M + (size_t)map * C.Mh + (size_t)i * C.pn + jp;  // + k*M
     const size_t dbase = ((size_t)(i * C.g + gam) * C.S_d) * C.R + map * C.pn + jp;               // + k*R
     const size_t coff = (size_t)sub * C.M * D + col, doff = (size_t)sub * C.R * D + col;
@@ -972,22 +1002,92 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedCombineParams C
       acc[e] = xor32_sum(acc[e]);
     }
     const float inv = L == 0.f ? 0.f : vs / L;  // no key seen: 0
-    y[map] = acc * inv;
+    return acc * inv;
+  };
+  const f32x4 y0 = merged(0), y1 = MAPS == 2 ? merged(1) : y0;
+  const u32x2 o = finish_row<D, MAPS>(C, j, y0, y1, col);
+  if (sub == 0) *reinterpret_cast<u32x2*>(C.out + (size_t)row * D + col) = o;
+}
+
+// ---------------------------------------------------------------------------
+// Small steps: work-group (sample, group) streams the unit's context and own
+// rows as one softmax and writes the output: one launch, no partials. The
+// context is read once per sample, so this pays where launches and latency set
+// the time.
+template <int D, typename KV, int NT, int MAPS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void whole_kernel(PagedWholeParams W) {
+  typedef StreamLds<D, KV> S;
+  constexpr int KS = D / 32, QB = q_bytes<D, NT>(), LPR = D / 4, RPW = 64 / LPR;
+  constexpr int LD = PageMerge<D, NT>::LD, ROWS = PageMerge<D, NT>::ROWS;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[QB + cmax(kWaves * S::TILE, PageMerge<D, NT>::bytes)];
+  const PagedAttnParams& P = W.A;
+  const PagedCombineParams& C = W.C;
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int gam = blockIdx.x % P.g, i = blockIdx.x / P.g;
+  unsigned char* kl = lds + QB + wave * S::TILE;
+  unsigned char* vl = kl + S::KT;
+  constexpr int stride = kWaves * kTileKeys;
+  const int k0 = wave * kTileKeys;
+  const int32_t* table = P.tables + (size_t)i * P.table_pages;
+  int c0 = 0, c1 = 0, o0 = 0, o1 = 0, raw = 0;  // first page ids, all requested together
+  if (P.m_c > 0) {
+    c0 = tile_ids(P.ctx_table, min(k0, P.m_c - 1), P.m_c, P.pool.shift, lane);
+    c1 = tile_ids(P.ctx_table, min(k0 + stride, P.m_c - 1), P.m_c, P.pool.shift, lane);
   }
-  f32x4 r = y[0];
-  if constexpr (MAPS == 2) {
-    r -= C.lambda[j / C.ntok] * y[1];
-    if (C.weight) {
-      float sq = r[0] * r[0] + r[1] * r[1] + r[2] * r[2] + r[3] * r[3];
-      if constexpr (LPR == 32) sq = xor16_sum(sq);
+  if (P.m_d_max > 0) {
+    o0 = tile_ids(table, min(k0, P.m_d_max - 1), P.m_d_max, P.pool.shift, lane);
+    o1 = tile_ids(table, min(k0 + stride, P.m_d_max - 1), P.m_d_max, P.pool.shift, lane);
+    raw = P.lens[i];
+  }
+  const OwnRows rows = {P.q + ((size_t)i * P.hn + (size_t)gam * P.pn) * D, D, P.R, P.pn};
+  u32x4 qreg[NT == 1 ? KS : 1];
+  if constexpr (NT == 1) {
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
-      const float f = 1.f / sqrtf(sq * (1.f / D) + C.eps);
-      r *= f * *reinterpret_cast<const f32x4*>(C.weight + col);
-    }
-    r *= C.out_scale;
+    for (int k = 0; k < KS; ++k) qreg[k] = query_slot<D, KV>(rows, 0, k, P.maps, P.q_sign, lane);
+  } else {
+    for (int k = wave; k < NT * KS; k += kWaves)
+      write128(lds + (k * 64 + lane) * 16, query_slot<D, KV>(rows, k / KS, k % KS, P.maps, P.q_sign, lane));
+    __syncthreads();
   }
-  if (sub == 0) *reinterpret_cast<u32x2*>(C.out + (size_t)row * D + col) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+  auto q_at = [&](int nt, int k) -> u32x4 {
+    if constexpr (NT == 1) return qreg[k];
+    return *(volatile const lds_u32x4*)(lds + ((nt * KS + k) * 64 + lane) * 16);
+  };
+  PageState<D, NT> st;
+  st.init();
+  const float sl2 = group_scale_log2(P, gam);
+  // the context's rows are read by the group's other samples too: cached
+  bool bad = stream_pages<D, NT, KV, 0>(st, P.pool, gam, P.ctx_table, q_at, kl, vl, c0, c1, k0, P.m_c, P.m_c, stride, 1,
+                                        sl2, lane);
+  const int total = __builtin_amdgcn_readfirstlane(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
+  bad |= stream_pages<D, NT, KV>(st, P.pool, gam, table, q_at, kl, vl, o0, o1, k0, total, total, stride, P.ntok, sl2, lane);
+  if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
+  total_sums(st);
+  float* merge = reinterpret_cast<float*>(lds + QB);
+  merge_states(st, merge, wave, lane);
+  const float* l_s = merge + ROWS * LD + ROWS;
+  const float vs = C.v_scale ? C.v_scale[gam] : 1.f;
+  const int sub = lane / LPR, col = 4 * (lane % LPR);
+  for (int r0 = wave * RPW; r0 < P.pn; r0 += kWaves * RPW) {
+    const int jp = r0 + sub, row = min(jp, P.pn - 1), j = gam * P.pn + row;
+    f32x4 y[MAPS];
+#pragma unroll
+    for (int u = 0; u < MAPS; ++u) {
+      const int r = u * P.pn + row;
+      const float L = l_s[r];
+      y[u] = *reinterpret_cast<const f32x4*>(merge + r * LD + col) * (L == 0.f ? 0.f : vs / L);
+    }
+    const u32x2 o = finish_row<D, MAPS>(C, j, y[0], y[MAPS - 1], col);
+    if (jp < P.pn) *reinterpret_cast<u32x2*>(C.out + ((size_t)i * P.hn + j) * D + col) = o;
+  }
+  if (threadIdx.x == 0) {
+    int flags = gam == 0 && P.m_d_max > 0 && (raw < 0 || raw > P.m_d_max) ? kStatusLens : 0;
+    if (i == 0) {
+      const float ks = C.k_scale ? C.k_scale[gam] : 1.f;
+      if (!(ks >= __FLT_MIN__ && ks <= __FLT_MAX__ && vs >= __FLT_MIN__ && vs <= __FLT_MAX__)) flags |= kStatusScale;
+    }
+    if (flags) atomicOr(P.status, flags);
+  }
 }
 
 template <typename Prm>
@@ -1048,7 +1148,32 @@ template <int D, int MAPS> hipError_t combine_dm(const PagedCombineParams& C, hi
                       : go(paged_combine_kernel<D, 16, MAPS>, grid, 256, s, stop, C);
 }
 
+template <int D, typename KV, int MAPS>
+hipError_t whole_dkm(const PagedWholeParams& W, int tiles, hipStream_t s, hipEvent_t stop) {
+  const int grid = W.A.b * W.A.g;
+  if (tiles == 1) return go(whole_kernel<D, KV, 1, MAPS>, grid, kThreads, s, stop, W);
+  if (tiles == 2) return go(whole_kernel<D, KV, 2, MAPS>, grid, kThreads, s, stop, W);
+  return hipErrorInvalidValue;
+}
+template <int D, typename KV>
+hipError_t whole_dk(const PagedWholeParams& W, int tiles, hipStream_t s, hipEvent_t stop) {
+  return W.A.maps == 2 ? whole_dkm<D, KV, 2>(W, tiles, s, stop) : whole_dkm<D, KV, 1>(W, tiles, s, stop);
+}
+
 }  // namespace
+
+hipError_t launch_paged_whole(const PagedWholeParams& W, int d, int kv, int tiles, hipStream_t s, hipEvent_t stop) {
+  if (d == 128) {
+    if (kv == kPagedBf16) return whole_dk<128, PgBf16>(W, tiles, s, stop);
+    if (kv == kPagedFp8) return whole_dk<128, PgFp8>(W, tiles, s, stop);
+    if (kv == kPagedMxfp4) return whole_dk<128, PgMx4>(W, tiles, s, stop);
+  } else if (d == 64) {
+    if (kv == kPagedBf16) return whole_dk<64, PgBf16>(W, tiles, s, stop);
+    if (kv == kPagedFp8) return whole_dk<64, PgFp8>(W, tiles, s, stop);
+    if (kv == kPagedMxfp4) return whole_dk<64, PgMx4>(W, tiles, s, stop);
+  }
+  return hipErrorInvalidValue;
+}
 
 hipError_t launch_paged_stream(const PagedAttnParams& P, int d, int kv, int tc, int td, hipStream_t s) {
   if (d == 128) {

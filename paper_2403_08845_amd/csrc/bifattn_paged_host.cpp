@@ -23,6 +23,7 @@ struct bifattn_paged_plan_s {
   int ctx_wide = 0;                  // many-row kernel: waves of a work-group, else 0
   int ctx_keys = 0, S_c = 0, ctx_row_blocks = 1, n_ctx_blocks = 0, n_ctx_small_blocks = 0;
   int dec_keys = 0, S_d = 0, n_dec_blocks = 0;
+  int whole = 0;                     // one launch, without partials (small steps)
   // The plan's own stream orders the workspace's allocation and freeing;
   // done_ev marks the end of its last call.
   hipStream_t own = nullptr;
@@ -161,6 +162,40 @@ ManySplit many_row_split(const bifattn_paged_plan_s* P) {
     }
   }
   return best;
+}
+
+// Whether a step runs as one launch without partials (whole_kernel): where the
+// estimate of its time, us, is below that of the parts and the combine. Both are
+// fits to 1500 random layers timed either way (up to 1536 units of at most 32
+// query rows, 4000 keys); over 1500 others the choice is 0.6% slower than the
+// faster way on average, 3% at the 95th percentile (always in parts: 21%).
+//   one launch: a start, the unit's keys, which take longer as units share a
+//     CU, and their bytes; never below a launch's own cost;
+//   in parts: a start, the longest work-group's keys, partials, work-groups
+//     beyond the GPU's slots, bytes; never below two launches'.
+bool takes_one_launch(const bifattn_paged_plan_s* P) {
+  const bifattn_paged_dims_t& d = P->dims;
+  const int64_t units = (int64_t)d.b * d.g;
+  const int env = env_int("BIFATTN_WHOLE", 0);  // 1: where it can, 2: never
+  if (P->dec_tiles > 2 || env == 2) return false;
+  if (env == 1) return true;
+  if (units > 1536 || (int64_t)d.m_c + d.m_d_max > 4000) return false;
+  const bool two = P->R > 16;
+  const double half = d.d == 64 ? 0.63 : 1.0;
+  const double key = (d.kv_type == BIFATTN_KV_MXFP4 ? 7.1e-3 : 8.4e-3) * half * (two ? 1.9 : 1.0);
+  const double row = 2.0 * paged_row_bytes(d.d, d.kv_type);
+  const double keys = (double)d.m_c + d.m_d_max;
+  const double one = std::max(7.4, 5.4 + (two ? 0.7 : 0.0) +
+                                       key * keys * (1.0 + 1.37 * std::max(0.0, (double)units / 402.0 - 1.0)) +
+                                       row * (double)units * keys / 17.3e6);
+  double parts = row * ((double)units * d.m_d_max + (double)d.g * d.m_c) / 5.4e6 +
+                 6.8e-7 * (double)(P->S_c + kWaves * P->S_d) * P->M * d.g * (d.d * 4 + 16) +
+                 1.4 * std::max(0.0, (double)(P->n_ctx_blocks + P->n_ctx_small_blocks + P->n_dec_blocks) / 512.0 - 1.0);
+  if (P->ctx_wide)
+    parts += 7.2 + 0.016 * half * P->ctx_keys;
+  else
+    parts += 7.2 + key * std::max(P->S_c ? (double)d.m_c / P->S_c : 0.0, (double)std::min(P->dec_keys, d.m_d_max));
+  return one <= std::max(8.7, parts);
 }
 
 bifattn_status_t split_work(bifattn_paged_plan_s* P) {
@@ -311,22 +346,6 @@ bifattn_status_t attend(bifattn_paged_plan_s* P, const void* q, const bifattn_pa
   // scale * (q . k) = |scale| * ((-q) . k): the kernels see a positive scale
   K.scale_log2 = std::fabs(P->scale) * 1.4426950408889634f;
   K.q_sign = P->scale < 0.f ? 0x80008000u : 0u;
-  hipError_t e = hipSuccess;
-  if (P->ctx_wide) {
-    // Units of more than 32 rows need more registers than two waves per SIMD
-    // have: their own rows follow in a launch of their own.
-    const bool one = P->dec_tiles <= 2;
-    K.n_ctx_blocks = P->n_ctx_blocks;
-    K.n_dec_blocks = one ? P->n_dec_blocks : 0;
-    e = launch_paged_wide(K, d.d, d.kv_type, P->dec_tiles, stream);
-    K.n_dec_blocks = one ? 0 : P->n_dec_blocks;
-    if (e == hipSuccess && K.n_dec_blocks) e = launch_paged_stream(K, d.d, d.kv_type, 0, P->dec_tiles, stream);
-  } else {
-    K.n_ctx_small_blocks = P->n_ctx_small_blocks;
-    K.n_dec_blocks = P->n_dec_blocks;
-    e = launch_paged_stream(K, d.d, d.kv_type, P->ctx_tiles, P->dec_tiles, stream);
-  }
-  if (e != hipSuccess) return BIFATTN_EHIP;
   PagedCombineParams C{};
   C.ctx_acc = P->ctx_acc;
   C.ctx_ml = P->ctx_ml;
@@ -353,6 +372,27 @@ bifattn_status_t attend(bifattn_paged_plan_s* P, const void* q, const bifattn_pa
   C.m_d_max = d.m_d_max;
   C.S_c = P->S_c;
   C.S_d = P->S_d * kWaves;
+  hipError_t e = hipSuccess;
+  if (P->whole) {
+    const PagedWholeParams W{K, C};
+    e = launch_paged_whole(W, d.d, d.kv_type, P->dec_tiles, stream, P->done_ev);
+    return e == hipSuccess ? BIFATTN_OK : BIFATTN_EHIP;
+  }
+  if (P->ctx_wide) {
+    // Units of more than 32 rows need more registers than two waves per SIMD
+    // have: their own rows follow in a launch of their own.
+    const bool one = P->dec_tiles <= 2;
+    K.n_ctx_blocks = P->n_ctx_blocks;
+    K.n_dec_blocks = one ? P->n_dec_blocks : 0;
+    e = launch_paged_wide(K, d.d, d.kv_type, P->dec_tiles, stream);
+    K.n_dec_blocks = one ? 0 : P->n_dec_blocks;
+    if (e == hipSuccess && K.n_dec_blocks) e = launch_paged_stream(K, d.d, d.kv_type, 0, P->dec_tiles, stream);
+  } else {
+    K.n_ctx_small_blocks = P->n_ctx_small_blocks;
+    K.n_dec_blocks = P->n_dec_blocks;
+    e = launch_paged_stream(K, d.d, d.kv_type, P->ctx_tiles, P->dec_tiles, stream);
+  }
+  if (e != hipSuccess) return BIFATTN_EHIP;
   return launch_paged_combine(C, d.d, stream, P->done_ev) == hipSuccess ? BIFATTN_OK : BIFATTN_EHIP;
 }
 
@@ -376,6 +416,7 @@ bifattn_status_t bifattn_paged_plan_create(const bifattn_paged_dims_t* dims, bif
     delete P;
     return st;
   }
+  P->whole = takes_one_launch(P);
   P->scale = dims->scale != 0.f ? dims->scale : 1.0f / std::sqrt((float)dims->d / (float)P->maps);
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1 || hipGetDevice(&P->device) != hipSuccess) {
@@ -439,7 +480,7 @@ bifattn_status_t bifattn_paged_plan_get_info(bifattn_paged_plan_t P, bifattn_pla
   info->dec_splits = P->S_d * kWaves;
   info->dec_blocks = P->n_dec_blocks;
   info->fused = !P->ctx_wide || P->dec_tiles <= 2;
-  info->path = BIFATTN_PATH_BIFURCATED;
+  info->path = P->whole ? BIFATTN_PATH_STANDARD : BIFATTN_PATH_BIFURCATED;
   info->workspace_bytes = P->ws_bytes;
   info->ctx_kernel = P->ctx_wide ? 2 : 0;
   return BIFATTN_OK;

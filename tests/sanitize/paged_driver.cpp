@@ -59,6 +59,9 @@ hipError_t launch_paged_wide(const PagedAttnParams& P, int, int, int td, hipStre
 hipError_t launch_paged_combine(const PagedCombineParams& C, int, hipStream_t, hipEvent_t) {
   return g_combine = C, g_launches |= 4, hipSuccess;
 }
+hipError_t launch_paged_whole(const PagedWholeParams& W, int, int, int tiles, hipStream_t, hipEvent_t) {
+  return g_stream = W.A, g_combine = W.C, g_dec_tiles = tiles, g_launches |= 32, hipSuccess;
+}
 hipError_t launch_paged_append(const PagedAppendParams& A, int, hipStream_t, hipEvent_t) {
   return g_append = A, g_launches |= 8, hipSuccess;
 }
@@ -280,7 +283,7 @@ static void splits() {
   auto pick = [&](int lo, int hi) { return (int)std::lround(std::exp(std::uniform_real_distribution<double>(std::log(lo), std::log(hi))(rng))); };
   alignas(16) static char mem[64];
   int32_t* i = (int32_t*)mem;
-  int seen = 0;
+  int seen = 0, whole = 0;
   while (seen < 4000) {
     bifattn_paged_dims_t d{};
     d.g = pick(1, 40), d.h = d.g * pick(1, 32), d.b = pick(1, 600), d.n = pick(1, 8), d.d = rng() % 2 ? 64 : 128;
@@ -300,6 +303,16 @@ static void splits() {
     const int R = d.maps * d.h / d.g * d.n, M = d.b * R;
     const int64_t units = (int64_t)d.b * d.g;
     const PagedCombineParams& C = g_combine;
+    bifattn_plan_info_t info;
+    CHECK(bifattn_paged_plan_get_info(P, &info) == BIFATTN_OK);
+    CHECK((info.path == BIFATTN_PATH_STANDARD) == (g_launches == 32));
+    if (g_launches == 32) {  // small steps: the unit fits two query tiles
+      CHECK(g_dec_tiles <= 2 && g_dec_tiles * 16 >= R && units <= 1536 && d.m_c + d.m_d_max <= 4000);
+      CHECK(g_stream.R == R && C.R == R && C.pn * d.maps == R && C.hn == d.h * d.n);
+      ++whole;
+      CHECK(bifattn_paged_plan_destroy(P) == BIFATTN_OK);
+      continue;
+    }
     const PagedAttnParams& K = g_launches & 2 ? g_wide : g_stream;
     CHECK(g_launches & 4);
     CHECK(K.R == R && K.M == M && K.M == K.maps * K.Mh && K.R == K.maps * K.pn && C.M == M && C.R == R);
@@ -344,6 +357,7 @@ static void splits() {
     CHECK(A.tickets + d.b == K.status && A.tokens_per_block <= 8);
     CHECK(bifattn_paged_plan_destroy(P) == BIFATTN_OK);
   }
+  CHECK(whole > 100 && whole < 3000);
 }
 
 int main() {

@@ -13,6 +13,13 @@ from .paged_ref import Problem
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True, params=["parts", "one launch"])
+def launches(request, monkeypatch):
+    """Every test runs in parts and, where a unit's rows fit, as one launch."""
+    monkeypatch.setenv("BIFATTN_WHOLE", "2" if request.param == "parts" else "1")
+    return request.param
+
+
 def attend(x, plan=None, pages=None, scale=None, lam=None, weight=None, eps=1e-5, out_scale=1.0, status=bif.OK,
            q=None, out=None):
     own = plan is None
@@ -230,6 +237,14 @@ def test_captured_steps_replay(case, maps):
             ref, tol = x.attention(lam=lam, q=q)
             assert ((got.cpu().double() - ref).abs() <= tol).all()
         assert bif.bifattn_paged_plan_status(plan) == bif.OK
+
+
+def test_small_steps_are_one_launch_by_estimate(monkeypatch):
+    monkeypatch.delenv("BIFATTN_WHOLE")
+    for dims, path in (((4, 4, 4, 64, 128, 16), "standard"), ((32, 32, 32, 128, 8192, 512), "bifurcated"),
+                       ((2, 64, 1, 128, 10, 10), "bifurcated")):  # 64 query rows per unit
+        with bif.PagedPlan(*dims, page=16, num_pages=9) as plan:
+            assert plan.info()["path"] == bif.PATHS[path]
 
 
 def test_two_plans_on_two_streams():
