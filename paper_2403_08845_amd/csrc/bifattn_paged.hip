@@ -100,6 +100,16 @@ template <int AUX> __device__ __forceinline__ uint32_t load_u8(__amdgpu_buffer_r
   return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, off, 0, AUX);
 }
 
+// A value that is the same in all lanes, in a scalar register. The statement
+// hides that it is: the compiler drops a readfirstlane of a value it knows to be
+// uniform and then, where a vector instruction made it (a vector load, a
+// three-way median), builds every buffer resource that depends on it lane by
+// lane, in a loop around each load.
+__device__ __forceinline__ int scalar(int x) {
+  asm("" : "+v"(x));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
 // Padded rows in LDS: 16 key rows of an operand read start in different
 // 16-byte bank groups, the 4 value rows of a transposing read in different
 // 32-byte ones.
@@ -139,7 +149,7 @@ template <int D, typename KV> struct PageTile {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
       const int id = a ? id1 : id0, key = key0 + 16 * a;
-      const int n = min(16, max(0, k1 - key));
+      const int n = scalar(min(16, max(0, k1 - key)));
       const size_t row = ((size_t)((int64_t)id * P.g + gam) << P.shift) + (key & ((1 << P.shift) - 1));
       const __amdgpu_buffer_rsrc_t rk = half_rsrc(P.K + row * RB, n, RB);
       const __amdgpu_buffer_rsrc_t rv = half_rsrc(P.V + row * RB, n, RB);
@@ -444,7 +454,7 @@ __device__ __forceinline__ void own_block(const PagedAttnParams& P, int blk, boo
     __syncthreads();
   }
   if (!on) return;
-  const int total = __builtin_amdgcn_readfirstlane(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
+  const int total = scalar(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
   auto q_at = [&](int nt, int k) -> u32x4 {
     if constexpr (NT == 1) return qreg[k];
     return *(volatile const lds_u32x4*)(qs + ((nt * KS + k) * 64 + lane) * 16);
@@ -1062,7 +1072,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // the context's rows are read by the group's other samples too: cached
   bool bad = stream_pages<D, NT, KV, 0>(st, P.pool, gam, P.ctx_table, q_at, kl, vl, c0, c1, k0, P.m_c, P.m_c, stride, 1,
                                         sl2, lane);
-  const int total = __builtin_amdgcn_readfirstlane(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
+  const int total = scalar(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
   bad |= stream_pages<D, NT, KV>(st, P.pool, gam, table, q_at, kl, vl, o0, o1, k0, total, total, stride, P.ntok, sl2, lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
