@@ -598,6 +598,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   stream_body<D, KV, NTC, NTD>(P);
 }
 template <int D, typename KV, int NTC, int NTD>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void stream_kernel_3w(PagedAttnParams P) {
+  stream_body<D, KV, NTC, NTD>(P);
+}
+template <int D, typename KV, int NTC, int NTD>
 __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
   stream_body<D, KV, NTC, NTD>(P);
 }
@@ -1125,7 +1129,14 @@ hipError_t stream_dk(const PagedAttnParams& P, int tc, int td, hipStream_t s) {
            : tc == 2 ? go(stream_kernel_2w<D, KV, 2, 2>, grid, kThreads, s, nullptr, P)
                      : hipErrorInvalidValue;
   if (td != 1) return hipErrorInvalidValue;
-  switch (tc) {
+  if constexpr (KV::MX) {
+    switch (tc) {
+      case 0: return go(stream_kernel_3w<D, KV, 0, 1>, grid, kThreads, s, nullptr, P);
+      case 1: return go(stream_kernel_3w<D, KV, 1, 1>, grid, kThreads, s, nullptr, P);
+      case 2: return go(stream_kernel_3w<D, KV, 2, 1>, grid, kThreads, s, nullptr, P);
+      default: return hipErrorInvalidValue;
+    }
+  } else switch (tc) {
     case 0: return go(stream_kernel_2w<D, KV, 0, 1>, grid, kThreads, s, nullptr, P);
     case 1: return go(stream_kernel_2w<D, KV, 1, 1>, grid, kThreads, s, nullptr, P);
     case 2: return go(stream_kernel_2w<D, KV, 2, 1>, grid, kThreads, s, nullptr, P);

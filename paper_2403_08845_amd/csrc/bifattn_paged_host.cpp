@@ -164,6 +164,40 @@ ManySplit many_row_split(const bifattn_paged_plan_s* P) {
   return best;
 }
 
+// Keys of a few-row context work-group: the least of an estimate of the step's
+// time. A step is as long as its longest work-group (whose keys take longer as
+// the GPU fills), the work over the slots, or the bytes, with the partials and
+// the combine behind it. The constants are a fit of whole steps: 1500 random
+// layers (up to 32 rows per group, 0.5k to 40k keys) at about nine chunks each;
+// over 1500 others the choice is 2.1% slower than the best chunk on average, 10%
+// at the 95th percentile (chunks of twice an even share over 512 slots, within
+// 256 and 2048: 4.4%, 16%).
+int64_t few_row_keys(const bifattn_paged_plan_s* P) {
+  const bifattn_paged_dims_t& d = P->dims;
+  const bool bf16 = d.kv_type == BIFATTN_KV_BF16, fp8 = d.kv_type == BIFATTN_KV_FP8_E4M3;
+  const double slots = kCUs * (bf16 ? 2.95 : fp8 ? 1.65 : 1.51) * (d.d == 64 ? 1.5 : 1.0);
+  const double key = (bf16 ? 7.4e-3 : fp8 ? 7.2e-3 : 6.6e-3) * (d.d == 64 ? 0.51 : 1.0);
+  const int64_t units = (int64_t)d.b * d.g;
+  const double td =
+      P->S_d ? 3.52 + key * (P->R > 16 ? 1.87 : 1.0) * (double)round_up(std::min(P->dec_keys, d.m_d_max), 128) : 0.0;
+  const double bytes = 2.0 * paged_row_bytes(d.d, d.kv_type) * ((double)d.g * d.m_c + 0.75 * (double)units * d.m_d_max);
+  int64_t best = 128;
+  double least = -1.0;
+  for (int64_t keys = 128; keys <= 2560; keys += keys < 768 ? 128 : keys < 1536 ? 256 : 512) {
+    const int64_t S = ceil_div(d.m_c, keys), wgs = d.g * S + units * P->S_d;
+    // whole tiles of the group's 4 S waves
+    const double tc = 3.52 + key * (P->M > 16 ? 1.87 : 1.0) * (double)(128 * ceil_div(d.m_c, 128 * S));
+    const double chain = std::max(tc, td);
+    const double filled = std::max(((double)d.g * S * tc + (double)units * P->S_d * td) / slots, bytes / 6.09e6);
+    const int64_t loads = ceil_div(S * d.d, 256) + ceil_div(4 * (int64_t)P->S_d * d.d, 256);
+    double t = std::max(chain * (1.0 + 0.24 * std::min(1.0, (double)wgs / slots)), filled) + 0.15 * std::min(chain, filled);
+    t += 8.1e-7 * (double)(S + kWaves * P->S_d) * P->M * d.g * (d.d * 4 + 16) +
+         P->maps * (1.58 * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3072 ? 8 : 16) - 1) + (loads > 8 ? 0.66 : 0.0));
+    if (least < 0.0 || t < least) least = t, best = keys;
+  }
+  return best;
+}
+
 // Whether a step runs as one launch without partials (whole_kernel): where the
 // estimate of its time, us, is below that of the parts and the combine. Both are
 // fits to 1500 random layers timed either way (up to 1536 units of at most 32
@@ -219,14 +253,7 @@ bifattn_status_t split_work(bifattn_paged_plan_s* P) {
   if (M <= 32 || (M <= 64 && P->dec_tiles == 4)) {
     P->ctx_tiles = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
     if (P->ctx_tiles < P->dec_tiles) P->ctx_tiles = P->dec_tiles;
-    // About four splits of 1024..2048 keys where the step fills the GPU;
-    // where it leaves slots idle, chunks of about twice an even share.
-    const int64_t longest =
-        std::min<int64_t>(2048, std::max<int64_t>(1024, round_up(ceil_div(d.m_c, 4), kWaves * kTileKeys)));
-    int64_t keys = longest;
-    const int64_t all = (int64_t)d.g * d.m_c + units * d.m_d_max;
-    const int64_t even = std::max<int64_t>(256, ceil_div(2 * all, 2 * kCUs));
-    if (even < keys) keys = round_up(ceil_div(d.m_c, ceil_div(d.m_c, even)), kWaves * kTileKeys);
+    const int64_t keys = few_row_keys(P);
     P->ctx_keys = (int)round_up(env_int("BIFATTN_CTX_KEYS", (int)keys), kWaves * kTileKeys);
     P->S_c = (int)ceil_div(d.m_c, P->ctx_keys);
     P->n_ctx_small_blocks = d.g * P->S_c;
