@@ -152,7 +152,7 @@ ManySplit many_row_split(const bifattn_paged_plan_s* P) {
       double t = (double)(wgs / slots) * tc + std::max(tr, beside) + 0.05 * std::min(tr, beside);
       t = std::max(t, bytes / 7.5e6);
       const int64_t loads = ceil_div(parts * d.d, 256) + ceil_div(4 * (int64_t)P->S_d * d.d, 256);
-      t += 1.66 * P->maps * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3072 ? 8 : 16) - 1) +
+      t += 1.66 * P->maps * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3 * 4 * kCUs ? 8 : 16) - 1) +
            (double)(parts + 4 * P->S_d) * P->M * d.g * (d.d * 4 + 16) / 2.1e6;
       if (least < 0.0 || t < least) {
         least = t;
@@ -192,7 +192,7 @@ int64_t few_row_keys(const bifattn_paged_plan_s* P) {
     const int64_t loads = ceil_div(S * d.d, 256) + ceil_div(4 * (int64_t)P->S_d * d.d, 256);
     double t = std::max(chain * (1.0 + 0.24 * std::min(1.0, (double)wgs / slots)), filled) + 0.15 * std::min(chain, filled);
     t += 8.1e-7 * (double)(S + kWaves * P->S_d) * P->M * d.g * (d.d * 4 + 16) +
-         P->maps * (1.58 * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3072 ? 8 : 16) - 1) + (loads > 8 ? 0.66 : 0.0));
+         P->maps * (1.58 * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3 * 4 * kCUs ? 8 : 16) - 1) + (loads > 8 ? 0.66 : 0.0));
     if (least < 0.0 || t < least) least = t, best = keys;
   }
   return best;
