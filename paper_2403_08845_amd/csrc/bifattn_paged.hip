@@ -29,6 +29,7 @@ namespace {
 typedef __attribute__((address_space(3))) unsigned char lds_u8;
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 
 constexpr int cmax(int a, int b) { return a > b ? a : b; }
 
@@ -245,11 +246,61 @@ __device__ __forceinline__ void split_weights(const float* pr, uint32_t* hi, uin
   }
 }
 
+// Whether a staged value tile holds an infinity or a NaN: the sum carries past
+// an exponent of all ones.
+template <int D> __device__ __forceinline__ bool has_odd_values(const unsigned char* vl, int lane) {
+  uint32_t odd = 0;
+#pragma unroll
+  for (int u = 0; u < kTileKeys * D / 512; ++u) {
+    const int at = 64 * u + lane;
+    const u32x4 v = *(volatile const lds_u32x4*)(vl + at / (D / 8) * PageRow<D>::VROW + at % (D / 8) * 16);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) odd |= (v[w] & 0x7f807f80u) + 0x00800080u;
+  }
+  return __any((odd & 0x80008000u) != 0);
+}
+
+// Keys of the tile from `first` on that hold such values, and that later tokens
+// alone see: their weight in the rows before is 0, which the products would
+// turn into NaN. They enter the rows that see them one by one and leave the tile.
+template <int D, int NT>
+__device__ __forceinline__ void take_odd_values(PageState<D, NT>& st, unsigned char* vl, const u32x4* hi, const u32x4* lo,
+                                             int first, int lane) {
+#pragma unroll 1
+  for (int key = first; key < kTileKeys; ++key) {
+    unsigned char* row = vl + key * PageRow<D>::VROW;
+    const u32x4 own = *(volatile const lds_u32x4*)(row + 16 * (lane % (D / 8)));
+    bool odd = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) odd |= ((((own[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0);
+    if (!__any(odd)) continue;
+    const int e = 4 * (key / 16) + key % 4, from = (lane & 15) + 16 * (key % 16 / 4);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      uint32_t a = 0, b = 0;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        if (w == e / 2) a = hi[nt][w], b = lo[nt][w];
+      const int up = e % 2 ? 0 : 16;
+      const float p = __shfl(__uint_as_float(a << up & 0xffff0000u) + __uint_as_float(b << up & 0xffff0000u), from);
+      if (!(p == 0.f))
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+          const u32x2 v = *(volatile const lds_u32x2*)(row + 32 * t + 8 * (lane >> 4));
+          st.acc[nt][t] += p * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xffff0000u),
+                                     __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xffff0000u)};
+        }
+    }
+    if (lane < D / 8) write128(row + 16 * lane, u32x4{0, 0, 0, 0});
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // One staged tile against NT query tiles. rem: keys from the tile's first to
 // the end of the sequence; row r sees keys < rem - (ntok - 1) + r % ntok.
 template <int D, int NT, typename KV, typename QAt>
 __device__ __forceinline__ void page_update(PageState<D, NT>& st, const PageTile<D, KV>& A,
-                                            const unsigned char* kl, const unsigned char* vl, QAt&& q_at,
+                                            const unsigned char* kl, unsigned char* vl, QAt&& q_at,
                                             int rem, int ntok, float scale_log2, int lane) {
   constexpr int KS = D / 32, DV = D / 16;
   const int G = lane >> 4;
@@ -316,6 +367,8 @@ __device__ __forceinline__ void page_update(PageState<D, NT>& st, const PageTile
     hi[nt] = u32x4{h[0], h[1], h[2], h[3]};
     lo[nt] = u32x4{o[0], o[1], o[2], o[3]};
   }
+  if (ntok > 1 && rem < kTileKeys + ntok - 1 && has_odd_values<D>(vl, lane))
+    take_odd_values<D, NT>(st, vl, hi, lo, max(0, rem - (ntok - 1)), lane);
 #pragma unroll
   for (int t = 0; t < DV; ++t) {
     const u32x4 v = PageTile<D, KV>::vop(vl, t, lane);
@@ -617,8 +670,9 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
 // Bound by the matrix cores, so code caches take fp16 for the value product:
 // one term of 11 bits for the weights (their error 2e-4 beside the output's
 // 1.7e-3) where bf16 values need two. E4M3 values are exact in fp16. MXFP4
-// values enter relative to the largest scale of the work-group's keys, read
-// ahead (1/16 of the chunk's value bytes), and are exact down to 2^-31 of it.
+// values enter relative to the largest scale of the same 32 elements among the
+// work-group's keys, read ahead (1/16 of the chunk's value bytes), and are exact
+// down to 2^-31 of it.
 template <int D, int NW, int SK, typename KV, int MAPS>
 __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigned char* lds) {
   constexpr int KD = D / MAPS;             // dims of the logits
@@ -680,7 +734,8 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
       if constexpr (KV::MX) ex[u] = ((is_v ? pool.V_exp : pool.K_exp) + at * EB)[c];
     }
   };
-  int vref = 0;  // MXFP4: exponent that the scales of the value rows are relative to
+  int vref = 0;  // MXFP4: exponent that the scales of this thread's chunk column of values are relative to
+  int vrefs[EB];  // of all columns
   auto stage_put = [&](int key0, int buf) {
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
@@ -712,21 +767,31 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   stage_get(0);
   if (SK < nkeys) get_ids(SK);
   if constexpr (KV::MX) {
-    // the largest scale byte that is a number; values then reach 6 * 2^8
-    int top = 0;
+    // the largest scale byte of each column that is a number; values then reach 6 * 2^8
+    static_assert(CPR == EB && (64 * NW) % EB == 0, "a chunk is a scale block, a thread's column stays");
+    int top[EB];
+#pragma unroll
+    for (int c = 0; c < EB; ++c) top[c] = 0;
     for (int key = threadIdx.x; key < nkeys; key += 64 * NW) {
       const uint8_t* e = pool.V_exp + row_of(k0 + key, P.ctx_table[(k0 + key) >> pool.shift]) * EB;
 #pragma unroll
-      for (int c = 0; c < EB; ++c) top = max(top, e[c] == 255 ? 0 : (int)e[c]);
+      for (int c = 0; c < EB; ++c) top[c] = max(top[c], e[c] == 255 ? 0 : (int)e[c]);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o));
     int* tops = reinterpret_cast<int*>(lds);
-    if (lane == 0) tops[wave] = top;
+#pragma unroll
+    for (int c = 0; c < EB; ++c) {
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) top[c] = max(top[c], __shfl_xor(top[c], o));
+      if (lane == 0) tops[wave * EB + c] = top[c];
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = max(top, tops[w]);
-    vref = __builtin_amdgcn_readfirstlane(top) - 127 - 8;
+    for (int c = 0; c < EB; ++c) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) top[c] = max(top[c], tops[w * EB + c]);
+      vrefs[c] = __builtin_amdgcn_readfirstlane(top[c]) - 127 - 8;
+      vref = (int)threadIdx.x % EB == c ? vrefs[c] : vref;
+    }
     __syncthreads();
   }
 
@@ -879,7 +944,7 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
 #pragma unroll
       for (int t = 0; t < DB; ++t)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vref);
+        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vrefs[t]);
     }
 #pragma unroll
     for (int t = 0; t < DB; ++t)

@@ -128,9 +128,19 @@ class Problem:
         2^-15 (two bf16 terms), by its 32-bit logits (d products each, exponent
         and conversions) and by the order of its 32-bit sums over the keys;
         magnitudes are those of the sums' terms. The output is rounded to bf16
-        once."""
+        once.
+
+        With codes in the pages and many query rows in a group the context's weights
+        are one fp16 term instead: half a step of 2^-10 of each weight, and below
+        fp16's normal range (2^-14) half a step of 2^-24, beside a chunk's largest
+        weight and sum of 1 at least. MXFP4 values then count relative to the
+        largest scale of their 32 elements in a chunk, which enters as 2^8: to half
+        a step of 2^-24, 2^-33 of that scale; the largest value there is at least
+        4 times it."""
         b, h, g, d, n, m_c, m_d = (getattr(self, k) for k in ("b", "h", "g", "d", "n", "m_c", "m_d"))
         w, p = d // self.maps, h // g
+        R, M = self.maps * p * n, self.maps * b * p * n
+        one_term = self.kv != "bf16" and (M > 64 or (M > 32 and R <= 32))
         scale = 1 / math.sqrt(w) if scale is None else scale
         q = (self.q if q is None else q).double().view(b, g, p, n, d)
         K, V = (torch.cat((self.ctx[x].expand(b, g, m_c, d), self.own[x]), 2)[:, :, None] for x in "KV")
@@ -148,8 +158,14 @@ class Problem:
             e = torch.exp(x - torch.where(top == -math.inf, 0.0, top))
             total = e.sum(-1, keepdim=True)
             e = torch.where(total > 0, e / total, 0.0)
-            tau = 2.0 ** -15 + EPS32 * (2 * (m_c + m_d) + 4 * (w + 16) * (size + 1))
-            maps.append((e @ V, tau * (e @ V.abs())))
+            tau = 2.0 ** -15 + (2.0 ** -11 if one_term else 0.0) + EPS32 * (2 * (m_c + m_d) + 4 * (w + 16) * (size + 1))
+            less = torch.zeros(())
+            if one_term and m_c:
+                less = 2.0 ** -25 * self.ctx["V"].abs().sum(1)[:, None, None]
+                if self.kv == "mxfp4":
+                    top = self.ctx["V"].abs().amax(1).unflatten(-1, (-1, 32)).amax(-1).repeat_interleave(32, -1)
+                    less = less + 2.0 ** -35 * top[:, None, None]
+            maps.append((e @ V, tau * (e @ V.abs()) + torch.where(total > 0, less, 0.0)))
         y, err = maps[0]
         if self.maps == 2:
             lam = lam.double().view(g, p, 1, 1)

@@ -275,3 +275,45 @@ def test_one_token_shapes():
         out = torch.zeros(x.b, x.h, x.d, dtype=torch.bfloat16, device="cuda")
         bif.bifattn_paged_decode(plan, x.q[:, :, 0].contiguous().cuda(), x.pages(), x.ctx_table.cuda(), x.tables.cuda(), x.lens.cuda(), out)
         assert torch.equal(out.cpu().double(), want[:, :, 0])
+
+
+@pytest.mark.parametrize("kv", ["bf16", "mxfp4"])
+@pytest.mark.parametrize("maps", [1, 2])
+@pytest.mark.parametrize("lens", [[70, 33, 64, 2], [5, 35, 3, 32]])
+def test_nonfinite_rows_of_later_tokens(lens, maps, kv):
+    """A draft token's infinite or NaN row reaches that token and the later ones
+    alone: the rows before it are as with any other value there."""
+    x = Problem(4, 6, 2, 128, 20, 70, n=4, page=16, kv=kv, maps=maps, lens=lens, seed=13)
+    lam = torch.full((x.h,), 0.5)
+    want = attend(x, lam=lam)
+    for back in (1, 3):  # the last token's row, the last but two's
+        bad = [int(v) - back for v in lens]
+        for i, t in enumerate(bad):
+            if t < 0:
+                continue
+            at = int(x.tables[i, t // 16]), t % 16
+            if kv == "mxfp4":
+                x.exps["V"][at[0], 1, at[1], 2] = x.exps["K"][at[0], 1, at[1], 0] = 255
+            else:
+                x.pool["V"][at[0], 1, at[1], 5:9] = torch.tensor([math.inf, -math.inf, math.nan, 1.0])
+                x.pool["K"][at[0], 1, at[1], 3] = math.nan
+        got = attend(x, lam=lam)
+        assert torch.equal(got[:, :3], want[:, :3])
+        for i, t in enumerate(bad):
+            first = x.n - (1 if t < 0 else back)  # the first token that sees a bad row
+            assert torch.equal(got[i, 3:, :first], want[i, 3:, :first])
+            assert torch.isnan(got[i, 3:, first:]).any(-1).all()
+
+
+def test_values_of_unlike_columns():
+    """MXFP4 value columns of very different size, in both context kernels: each
+    column of 32 elements keeps its own precision."""
+    for b in (2, 40):
+        x = Problem(b, 8, 2, 128, 300, 20, page=16, kv="mxfp4", lens=[20] * b, seed=14)
+        for name, tab, n in (("ctx", x.ctx_table.view(1, -1), [300]), ("own", x.tables, [20] * b)):
+            v = getattr(x, name)["V"] * torch.tensor([1.0, 2.0 ** 40, 2.0 ** -50, 2.0 ** 90]).repeat_interleave(32).double()
+            got = x._put("V", v if name == "own" else v[None], tab, torch.tensor(n), None)
+            getattr(x, name)["V"] = got if name == "own" else got[0]
+        got = attend(x)
+        ref, tol = x.attention()
+        assert ((got - ref).abs() <= tol).all()
