@@ -997,18 +997,18 @@ __device__ __forceinline__ u32x2 finish_row(const PagedCombineParams& C, int j, 
 }
 
 // ---------------------------------------------------------------------------
-// Combine: a wave per output row merges the row's partials (of each map) into
+// Combine: a wave per output row (and map) merges the row's partials into
 //   softmax @ V = vs sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k
-// (0 where no key was seen), subtracts the maps, normalises the head and rounds
-// the result to bf16 once. 16 bytes of a value row per lane, so a load reads
+// (0 where no key was seen); the maps meet in LDS, and the first one's wave
+// subtracts them, normalises the head and rounds the result to bf16 once. 16 bytes of a value row per lane, so a load reads
 // 256/D partials' rows; NL loads are issued ahead with the statistics.
 template <int D, int NL, int MAPS>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedCombineParams C) {
   constexpr int LPR = D / 4, PPL = 64 / LPR;
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int sub = lane / LPR, col = 4 * (lane % LPR);
-  const int row = blockIdx.x * 4 + wave;
-  if (row >= C.b * C.hn) return;
+  const int map = MAPS == 2 ? wave & 1 : 0;
+  const int at = blockIdx.x * (4 / MAPS) + wave / MAPS, row = min(at, C.b * C.hn - 1);
   const int i = row / C.hn, j = row - i * C.hn;
   const int gam = j / C.pn, jp = j - gam * C.pn;
   if (j == 0 && lane == 0 && C.lens) {
@@ -1022,7 +1022,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedCombineParams C
     if (!ok) atomicOr(C.status, kStatusScale);
   }
   const int np = C.S_c + C.S_d;
-  auto merged = [&](int map) {
+  auto merged = [&]() {
     const size_t cbase = (size_t)gam * C.S_c * C.M + (size_t)map * C.Mh + (size_t)i * C.pn + jp;  // + k*M
     const size_t dbase = ((size_t)(i * C.g + gam) * C.S_d) * C.R + map * C.pn + jp;               // + k*R
     const size_t coff = (size_t)sub * C.M * D + col, doff = (size_t)sub * C.R * D + col;
@@ -1086,9 +1086,16 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedCombineParams C
     const float inv = L == 0.f ? 0.f : vs / L;  // no key seen: 0
     return acc * inv;
   };
-  const f32x4 y0 = merged(0), y1 = MAPS == 2 ? merged(1) : y0;
+  const f32x4 y0 = merged();
+  f32x4 y1 = y0;
+  if constexpr (MAPS == 2) {
+    __shared__ f32x4 second[2][LPR];
+    if (map == 1 && sub == 0) second[wave / 2][lane] = y0;
+    __syncthreads();
+    y1 = second[wave / 2][lane % LPR];
+  }
   const u32x2 o = finish_row<D, MAPS>(C, j, y0, y1, col);
-  if (sub == 0) *reinterpret_cast<u32x2*>(C.out + (size_t)row * D + col) = o;
+  if (map == 0 && sub == 0 && at < C.b * C.hn) *reinterpret_cast<u32x2*>(C.out + (size_t)row * D + col) = o;
 }
 
 // ---------------------------------------------------------------------------
@@ -1226,7 +1233,7 @@ template <int D, typename KV> hipError_t many_dk(const PagedAttnParams& P, int t
 }
 
 template <int D, int MAPS> hipError_t combine_dm(const PagedCombineParams& C, hipStream_t s, hipEvent_t stop) {
-  const int grid = (C.b * C.hn + 3) / 4, per = 256 / D;
+  const int rows = 4 / MAPS, grid = (C.b * C.hn + rows - 1) / rows, per = 256 / D;
   const int loads = (C.S_c + per - 1) / per + (C.S_d + per - 1) / per;
   // All of a row's loads at once need registers that leave three waves per SIMD:
   // only where that holds every row (4096 rows of 17 partials: 10.5 us, 7.1 in
