@@ -401,7 +401,7 @@ bifattn_status_t bifattn_paged_plan_status(bifattn_paged_plan_t plan, hipStream_
  * parts of one projection's output; elements of a row are consecutive. */
 typedef struct {
   int32_t samples;  /* sequences the tokens go to: 1..b (context: 1) */
-  int32_t n;        /* tokens per sequence, >= 1 */
+  int32_t n;        /* tokens per sequence, 1..2^29 */
   int32_t context;  /* 0: the samples' own rows; 1: the shared context's */
   int32_t rot;      /* rotated elements of a head (of each half with maps = 2): a multiple of 16
                        up to d/maps; 0: none */
@@ -425,7 +425,8 @@ typedef struct {
  * nearest E2M1 values, ties to even, saturated at 6; a block that holds an
  * infinity or a NaN becomes NaN. q may overlap nothing that is written.
  *   lens_out[i] = lens[i] + counts[i]
- * lens_out may be lens (advanced in place). Rows past the sequence's capacity
+ * lens_out may be lens (advanced in place); otherwise the two do not overlap.
+ * Rows past the sequence's capacity
  * (m_c or m_d_max) are dropped, the length stops there, a length outside its
  * range is clamped first; all raise the ELENS flag. q_out rows of tokens past
  * counts[i] are left as they were. table [samples][ceil(capacity / page)].
@@ -475,7 +476,8 @@ bifattn_status_t bifattn_paged_decode(bifattn_paged_plan_t plan, const void *q,
  *   y = (softmax(scale * q1 . K1) - lambda[j] * softmax(scale * q2 . K2)) @ V
  *   out = out_scale * y,  or with weight (fp32 [d]):
  *   out = out_scale * weight * y / sqrt(mean(y^2) + eps)
- * lambda: fp32 [h]; eps >= 0. Everything else as in bifattn_paged_decode.
+ * (0 where y is 0 throughout, whatever eps). lambda: fp32 [h]; eps >= 0; the
+ * norm is formed in 32 bits. Everything else as in bifattn_paged_decode.
  */
 bifattn_status_t bifattn_paged_decode_diff(bifattn_paged_plan_t plan, const void *q,
                                            const bifattn_pages_t *pages, const int32_t *ctx_table,

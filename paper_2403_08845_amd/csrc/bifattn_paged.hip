@@ -989,7 +989,8 @@ __device__ __forceinline__ u32x2 finish_row(const PagedCombineParams& C, int j, 
       if constexpr (D == 128) sq = xor16_sum(sq);
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
-      r *= *reinterpret_cast<const f32x4*>(C.weight + col) / sqrtf(sq * (1.f / D) + C.eps);
+      const float mean = sq * (1.f / D) + C.eps;  // 0: a row of zeros, which stays one
+      r *= *reinterpret_cast<const f32x4*>(C.weight + col) * (mean == 0.f ? 0.f : 1.f / sqrtf(mean));
     }
     r *= C.out_scale;
   }

@@ -256,6 +256,7 @@ bifattn_status_t split_work(bifattn_paged_plan_s* P) {
     const int64_t keys = few_row_keys(P);
     P->ctx_keys = (int)round_up(env_int("BIFATTN_CTX_KEYS", (int)keys), kWaves * kTileKeys);
     P->S_c = (int)ceil_div(d.m_c, P->ctx_keys);
+    if ((int64_t)d.g * P->S_c > INT32_MAX / 4) return BIFATTN_EINVAL;
     P->n_ctx_small_blocks = d.g * P->S_c;
   } else {
     ManySplit split = many_row_split(P);
@@ -532,7 +533,7 @@ bifattn_status_t bifattn_paged_append(bifattn_paged_plan_t P, const bifattn_page
   bifattn_status_t st = check_pages(P, pages, &A.pool);
   if (st == BIFATTN_EINVAL) return st;
   A.max_rows = capacity(P, rows->context);
-  if (rows->samples < 1 || rows->samples > (rows->context ? 1 : d.b) || rows->n < 1 || A.max_rows < 1 ||
+  if (rows->samples < 1 || rows->samples > (rows->context ? 1 : d.b) || rows->n < 1 || rows->n > (1 << 29) || A.max_rows < 1 ||
       (rows->q != nullptr) != (rows->q_out != nullptr) || rows->rot < 0 || rows->rot > d.d / P->maps ||
       (rows->rot > 0 && !rows->freqs) || !on_plan_device(P, stream))
     return BIFATTN_EINVAL;

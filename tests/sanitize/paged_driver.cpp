@@ -215,6 +215,7 @@ static void refused_calls() {
       CHECK(app([](R& x) { x.context = 1; }) == BIFATTN_EINVAL);
       CHECK(app([](R& x) { x.samples = 4; }) == BIFATTN_EINVAL);
       CHECK(app([](R& x) { x.samples = 0; }) == BIFATTN_EINVAL);
+      CHECK(app([](R& x) { x.n = (1 << 29) + 1; }) == BIFATTN_EINVAL);
       CHECK(app([](R& x) { x.n = 0; }) == BIFATTN_EINVAL);
       CHECK(app([](R& x) { x.k = nullptr; }) == BIFATTN_EINVAL);
       CHECK(app([](R& x) { x.v = nullptr; }) == BIFATTN_EINVAL);

@@ -317,3 +317,13 @@ def test_values_of_unlike_columns():
         got = attend(x)
         ref, tol = x.attention()
         assert ((got - ref).abs() <= tol).all()
+
+
+def test_norm_without_eps_of_a_row_of_zeros():
+    """A token that sees no key stays 0 under the norm, with eps = 0 too."""
+    x = Problem(3, 8, 2, 128, 0, 40, page=32, maps=2, lens=[0, 7, 40], seed=15)
+    lam, weight = torch.full((x.h,), 0.5), torch.randn(x.d, generator=x.rng)
+    got = attend(x, lam=lam, weight=weight, eps=0.0)
+    assert (got[0] == 0).all()
+    ref, tol = x.attention(lam=lam, weight=weight, eps=0.0)
+    assert ((got - ref).abs() <= tol)[1:].all()
