@@ -97,6 +97,12 @@ bifattn_status_t check_dims(const bifattn_paged_dims_t* d) {
   return BIFATTN_OK;
 }
 
+// Partials' loads that a combine wave issues together, at most (three work-groups
+// of four waves per CU hold 16).
+int64_t combine_loads(const bifattn_paged_plan_s* P) {
+  return (int64_t)P->maps * P->dims.b * P->dims.h * P->ntok > 12 * kCUs ? 8 : 16;
+}
+
 // Keys of an own-row work-group: the whole capacity up to 1024 keys, halved
 // (not below 256) while fewer than half as many work-groups as CUs would exist.
 int own_chunk(int64_t units, int64_t rows) {
@@ -111,8 +117,8 @@ int own_chunk(int64_t units, int64_t rows) {
 // own-row work-groups beside the last round of context ones, the partials and
 // the combine's loads), its constants a fit of whole steps: 1500 random layers
 // (33 to 10^4 rows per group, 0.1k to 40k keys, every type, both head kinds) at
-// about ten settings each. Over 1500 others the choice is 1.6% slower than the
-// best of those settings on average, 8% at the 95th percentile, 22% at worst; a fixed number
+// about ten settings each. Over 1500 others the choice is 1.8% slower than the
+// best of those settings on average, 8% at the 95th percentile, 29% at worst; a fixed number
 // of work-groups (160 of eight waves, 256 of four) 12%, 37% and up to 2.8 times.
 struct ManySplit {
   int waves = 4;
@@ -152,7 +158,7 @@ ManySplit many_row_split(const bifattn_paged_plan_s* P) {
       double t = (double)(wgs / slots) * tc + std::max(tr, beside) + 0.05 * std::min(tr, beside);
       t = std::max(t, bytes / 7.5e6);
       const int64_t loads = ceil_div(parts * d.d, 256) + ceil_div(4 * (int64_t)P->S_d * d.d, 256);
-      t += 1.66 * P->maps * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3 * 4 * kCUs ? 8 : 16) - 1) +
+      t += 1.66 * (double)(ceil_div(loads, combine_loads(P)) - 1) +
            (double)(parts + 4 * P->S_d) * P->M * d.g * (d.d * 4 + 16) / 2.1e6;
       if (least < 0.0 || t < least) {
         least = t;
@@ -192,7 +198,7 @@ int64_t few_row_keys(const bifattn_paged_plan_s* P) {
     const int64_t loads = ceil_div(S * d.d, 256) + ceil_div(4 * (int64_t)P->S_d * d.d, 256);
     double t = std::max(chain * (1.0 + 0.24 * std::min(1.0, (double)wgs / slots)), filled) + 0.15 * std::min(chain, filled);
     t += 8.1e-7 * (double)(S + kWaves * P->S_d) * P->M * d.g * (d.d * 4 + 16) +
-         P->maps * (1.58 * (double)(ceil_div(loads, (int64_t)d.b * d.h * P->ntok > 3 * 4 * kCUs ? 8 : 16) - 1) + (loads > 8 ? 0.66 : 0.0));
+         1.58 * (double)(ceil_div(loads, combine_loads(P)) - 1) + (loads > 8 ? 0.66 : 0.0);
     if (least < 0.0 || t < least) least = t, best = keys;
   }
   return best;
@@ -215,18 +221,19 @@ bool takes_one_launch(const bifattn_paged_plan_s* P) {
   if (env == 1) return true;
   if (units > 1536 || (int64_t)d.m_c + d.m_d_max > 4000) return false;
   const bool two = P->R > 16;
-  const double half = d.d == 64 ? 0.63 : 1.0;
-  const double key = (d.kv_type == BIFATTN_KV_MXFP4 ? 7.1e-3 : 8.4e-3) * half * (two ? 1.9 : 1.0);
+  const double half = d.d == 64 ? 0.52 : 1.0;
+  const double code = d.kv_type == BIFATTN_KV_BF16 ? 7.4e-3 : d.kv_type == BIFATTN_KV_FP8_E4M3 ? 8.0e-3 : 7.6e-3;
+  const double key = code * half * (two ? 1.7 : 1.0);
   const double row = 2.0 * paged_row_bytes(d.d, d.kv_type);
   const double keys = (double)d.m_c + d.m_d_max;
-  const double one = std::max(7.4, 5.4 + (two ? 0.7 : 0.0) +
-                                       key * keys * (1.0 + 1.37 * std::max(0.0, (double)units / 402.0 - 1.0)) +
-                                       row * (double)units * keys / 17.3e6);
-  double parts = row * ((double)units * d.m_d_max + (double)d.g * d.m_c) / 5.4e6 +
-                 6.8e-7 * (double)(P->S_c + kWaves * P->S_d) * P->M * d.g * (d.d * 4 + 16) +
-                 1.4 * std::max(0.0, (double)(P->n_ctx_blocks + P->n_ctx_small_blocks + P->n_dec_blocks) / 512.0 - 1.0);
+  const double one = std::max(6.5, 5.4 + (two ? 0.6 : 0.0) +
+                                       key * keys * (1.0 + 1.84 * std::max(0.0, (double)units / 368.0 - 1.0)) +
+                                       row * (double)units * keys / 26.5e6);
+  double parts = row * ((double)units * d.m_d_max + (double)d.g * d.m_c) / 10.3e6 +
+                 6.7e-7 * (double)(P->S_c + kWaves * P->S_d) * P->M * d.g * (d.d * 4 + 16) +
+                 1.1 * std::max(0.0, (double)(P->n_ctx_blocks + P->n_ctx_small_blocks + P->n_dec_blocks) / 512.0 - 1.0);
   if (P->ctx_wide)
-    parts += 7.2 + 0.016 * half * P->ctx_keys;
+    parts += 7.7 + 0.023 * half * P->ctx_keys;
   else
     parts += 7.2 + key * std::max(P->S_c ? (double)d.m_c / P->S_c : 0.0, (double)std::min(P->dec_keys, d.m_d_max));
   return one <= std::max(8.7, parts);
