@@ -852,9 +852,13 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
       f32x16 sacc;
 #pragma unroll
       for (int v = 0; v < 16; ++v) sacc[v] = 0.f;
+      // The wave in its products goes first, so that the other one of the SIMD
+      // does its softmax meanwhile (multi-query layer over 16k in fp8: 57 us, so 55).
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) sacc = mfma32(kw[ks], qop[ks], sacc);
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
       u32x4 vw[2][DB];
 #pragma unroll
       for (int ss = 0; ss < 2; ++ss)
@@ -919,6 +923,7 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
         lo[ss] = u32x4{l4[0], l4[1], l4[2], l4[3]};
       }
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
       if (b + 1 < SK / 32)
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) kw[ks] = read128(kb + 32 * (b + 1) * KROW + 32 * ks);
