@@ -125,8 +125,10 @@ __device__ __forceinline__ void widen8(const u32x4& r, float* f) {
 // are off by 2^-22 of themselves before their one rounding, codes are formed
 // from 64 bits.
 //
-// Byte work where the batch is large; a step of some tokens is one launch's
-// latency (a chain of loads: length, table entry, row).
+// Byte work where the batch is large (8192 tokens of 32 + 8 heads into MXFP4:
+// 46 us for 177 MB, 3.8 TB/s, of which a copy takes 35); a step of some tokens is
+// one launch's latency (a chain of loads: length, table entry, row; 32 samples of
+// 32 heads 4.4 us).
 template <int D, int KV>
 __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(4))) void append_kernel(PagedAppendParams A) {
   constexpr int TPR = D / 16;                       // threads of a row
@@ -252,7 +254,8 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
 }
 
 // Read-out: a thread's 8 elements of a row, widened (times the group's scale)
-// to bf16. Rows at or past a sample's length are not written.
+// to bf16. Rows at or past a sample's length are not written. Bytes alone: 8192
+// rows of 8 heads from MXFP4 9.3 us for 43 MB, 4.6 TB/s.
 template <int D, int KV>
 __global__ __launch_bounds__(256) void gather_kernel(PagedGatherParams P) {
   constexpr int C = D / 8, RB = paged_row_bytes(D, KV), EB = D / kMxBlock;
