@@ -111,14 +111,12 @@ __device__ __forceinline__ int scalar(int x) {
   return __builtin_amdgcn_readfirstlane(x);
 }
 
-// Padded rows in LDS, which serves 32 lanes from 64 banks at a time: 16 key rows
-// of an operand read start in different 16-byte bank groups; the value rows of a
-// transposing read by 32 lanes (8 rows of 32 bytes in the streaming waves, 4 of
-// 64 in the many-row kernel) do not meet in a bank.
+// Padded rows in LDS: 16 key rows of an operand read start in different
+// 16-byte bank groups, the 4 value rows of a transposing read in different
+// 32-byte ones.
 template <int D> struct PageRow {
   static constexpr int KROW = 2 * D + 16;
   static constexpr int VROW = 2 * D + 32;
-  static constexpr int WIDE_VROW = 2 * D + 64;
 };
 
 // Buffer resource over n rows of row_bytes from `base`; past them loads return
@@ -687,7 +685,7 @@ template <int D, int NW, int SK, typename KV, int MAPS>
 __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigned char* lds) {
   constexpr int KD = D / MAPS;             // dims of the logits
   constexpr int KSTEPS = KD / 16, DB = D / 32;
-  constexpr int KROW = PageRow<D>::KROW, VROW = PageRow<D>::WIDE_VROW;
+  constexpr int KROW = PageRow<D>::KROW, VROW = PageRow<D>::VROW;
   constexpr int STAGE = SK * (KROW + VROW);
   constexpr int RB = D * KV::BITS / 8, CPR = RB / 16, EB = D / kMxBlock;
   constexpr int LOADS = 2 * SK * CPR, PER = LOADS / (64 * NW);
@@ -978,7 +976,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
   typedef StreamLds<D, KV> S;
   constexpr int QB = q_bytes<D, NTD>();
   constexpr int UNITS = NW / kWaves;
-  constexpr int CTX = 2 * SK * (PageRow<D>::KROW + PageRow<D>::WIDE_VROW);
+  constexpr int CTX = 2 * SK * (PageRow<D>::KROW + PageRow<D>::VROW);
   __shared__ __attribute__((aligned(16))) unsigned char lds[cmax(CTX, UNITS * QB + NW * S::TILE)];
   const int bid = blockIdx.x;
   if (bid < P.n_ctx_blocks) {
