@@ -327,3 +327,52 @@ def test_norm_without_eps_of_a_row_of_zeros():
     assert (got[0] == 0).all()
     ref, tol = x.attention(lam=lam, weight=weight, eps=0.0)
     assert ((got - ref).abs() <= tol)[1:].all()
+
+
+def test_nonfinite_rows_of_many_draft_tokens():
+    """As above with 40 tokens, whose hidden rows span two tiles, in fp8."""
+    x = Problem(2, 2, 2, 64, 20, 90, n=40, page=16, kv="fp8_e4m3", lens=[90, 41], seed=16)
+    want = attend(x)
+    for i, length in enumerate((90, 41)):
+        for t in (length - 1, length - 33):  # of the last token, of the 8th
+            at = int(x.tables[i, t // 16]), t % 16
+            x.pool["V"][at[0], 0, at[1], 7] = 0x7F
+    got = attend(x)
+    assert torch.equal(got[:, 1], want[:, 1]) and torch.equal(got[:, 0, :7], want[:, 0, :7])
+    assert torch.isnan(got[:, 0, 7:, 7]).all()
+    rest = torch.arange(64) != 7
+    ref, tol = x.attention()
+    assert ((got - ref).abs() <= tol)[:, 0, 7:, rest].all()
+
+
+def test_two_parts_of_one_step_in_a_graph_with_a_second_plan():
+    """Two plans' steps in one captured graph, replayed: each has a workspace of
+    its own."""
+    x = Problem(5, 32, 4, 128, 515, 65, 2, 16, "bf16", seed=30)
+    y = Problem(3, 8, 2, 128, 77, 40, 1, 32, "mxfp4", seed=31)
+    want = [attend(x), attend(y)]
+    plans = [x.plan(), y.plan()]
+    args = [(z.q.cuda(), z.pages(), z.ctx_table.cuda(), z.tables.cuda(), z.lens.cuda()) for z in (x, y)]
+    outs = [torch.zeros(z.b, z.h, z.n, z.d, dtype=torch.bfloat16, device="cuda") for z in (x, y)]
+    side = torch.cuda.Stream()
+
+    def step():
+        for plan, a, out in zip(plans, args, outs):
+            bif.bifattn_paged_decode(plan, *a, out)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for _ in range(4):
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert torch.equal(out.cpu().double(), w)
+    for plan in plans:
+        plan.close()
