@@ -677,7 +677,14 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
 // over 32k rows in MXFP4: 176 us a step, 790 TFLOP/s). Code caches take fp16 for the
 // value product:
 // one term of 11 bits for the weights (their error 2e-4 beside the output's
-// 1.7e-3) where bf16 values need two. E4M3 values are exact in fp16. MXFP4
+// 1.7e-3) where bf16 values need two. The weights enter 2^kUp times as large, so
+// that fp16's range lies where theirs does: with a slack of 2^5 above the reference
+// they keep 11 bits down to 2^-24 of the row's largest among the work-group's keys;
+// below, a fixed step of 2^-34 of it. A smaller slack reaches further and raises
+// more often: grouped layer over 32k in MXFP4, multi-query one over 16k in fp8 and
+// grouped differential one over 16k in MXFP4 in turn 180, 58 and 37.3 us with 8, 180.5,
+// 58 and 37.4 with 5, 182, 60 and 38.0 with 4, 193, 66 and 43.6 with 2. E4M3 values
+// are exact in fp16. MXFP4
 // values enter relative to the largest scale of the same 32 elements among the
 // work-group's keys, read ahead (1/16 of the chunk's value bytes), and are exact
 // down to 2^-31 of it.
@@ -703,7 +710,9 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   const PagePool& pool = P.pool;
   const int mask = (1 << pool.shift) - 1;
   bool bad = false;
-  constexpr bool kHalf = KV::BITS < 16;  // values and weights in fp16
+  constexpr bool kHalf = KV::BITS < 16;  // values and weights in fp16, weights below 2^(kUp + kSlack)
+  constexpr float kUp = kHalf ? 10.f : 0.f, kSlack = kHalf ? 5.f : kRescaleSlack;
+  constexpr float kBound = kHalf ? 0x1p15f : kSumBound;  // 2^(kUp + kSlack)
   auto row_of = [&](int key, int id) {  // pool row of a context key, by its page id
     const bool wrong = (unsigned)id >= (unsigned)pool.num_pages;
     bad |= wrong;
@@ -889,10 +898,10 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
           if (8 * (v / 4) + 4 * h + (v & 3) >= nv) x[v] = kNegInf;
       }
       // Weights against the current reference first; a raise needs a weight
-      // above 2^kRescaleSlack, which shows in their sum.
+      // above 2^kSlack (times 2^kUp), which shows in their sum.
       float pr[16], ps;
       auto weights = [&]() {
-        const float nbase = mref == kNegInf ? 0.f : -mref;
+        const float nbase = mref == kNegInf ? 0.f : kUp - mref;
 #pragma unroll
         for (int v = 0; v < 16; ++v) pr[v] = exp2_fast(__builtin_fmaf(x[v], sl2, nbase));
         ps = pr[0];
@@ -900,12 +909,12 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
         for (int v = 1; v < 16; ++v) ps += pr[v];
       };
       weights();
-      if (__any(!(ps <= kSumBound) || mref == kNegInf)) {
+      if (__any(!(ps <= kBound) || mref == kNegInf)) {
         float lmax = x[0];
 #pragma unroll
         for (int v = 1; v < 16; ++v) lmax = fmaxf(lmax, x[v]);
         const float tmax = xor32_max(lmax) * sl2;
-        const bool raise = tmax > mref + kRescaleSlack;
+        const bool raise = tmax > mref + kSlack;
         if (__any(raise)) {
           const float alpha = raise ? exp2_fast(mref - tmax) : 1.f;
           lsum *= alpha;
@@ -949,7 +958,8 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   }
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   if (!active) return;
-  const float ltot = xor32_sum(lsum);
+  const float down = kHalf ? 0x1p-10f : 1.f;  // 2^-kUp
+  const float ltot = xor32_sum(lsum) * down;
   const int row = row0 + j;
   if (row < Mh) {
     const size_t prow = ((size_t)gam * P.S_c + s) * P.M + (size_t)map * Mh + row;
@@ -958,7 +968,10 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
 #pragma unroll
       for (int t = 0; t < DB; ++t)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vrefs[t]);
+        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vrefs[t] - (int)kUp);
+    } else if constexpr (kHalf) {
+#pragma unroll
+      for (int t = 0; t < DB; ++t) acc[t] *= down;
     }
 #pragma unroll
     for (int t = 0; t < DB; ++t)

@@ -1,0 +1,110 @@
+"""Paged caches where fewer bits would show: context weights far below the
+largest one, values far below the largest of their column, elements next to a
+border between codes, results of a rotation that cancel, norms of tiny and huge
+heads (MI355X only)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2403_08845_amd as bif
+
+from .paged_ref import EPS32, HALF_BF16, Problem, rotated
+from .test_paged_gpu import attend
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def in_parts(monkeypatch):
+    monkeypatch.setenv("BIFATTN_WHOLE", "2")
+
+
+def bounds(x, lam=None):
+    """(out, tolerance) float64: every weight is off by half a step of 11 bits (the
+    context's with codes and many rows; 2^-15 and less elsewhere) and, below 2^-24
+    of the largest weight, by half a step of 2^-34 of it (an fp16 step of 2^-24
+    where the largest is 2^10); by its 32-bit logit (w products, exponent and
+    conversions) and the order of the 32-bit sums over the keys; the output by
+    half a bf16 step."""
+    b, h, g, d, n, m_c, m_d = (getattr(x, k) for k in ("b", "h", "g", "d", "n", "m_c", "m_d"))
+    w, p = d // x.maps, h // g
+    q = x.q.double().view(b, g, p, n, d)
+    K, V = (torch.cat((x.ctx[k].expand(b, g, m_c, d), x.own[k]), 2)[:, :, None] for k in "KV")
+    pos = torch.arange(m_c + m_d)
+    seen = (pos < m_c + (x.lens.view(-1, 1, 1) - n + 1 + torch.arange(n).view(-1, 1)).clamp(min=0))[:, None, None]
+    V = torch.where((pos < m_c + x.lens.view(-1, 1))[:, None, None, :, None], V, 0.0)
+    maps = []
+    for u in range(x.maps):
+        f = slice(u * w, (u + 1) * w)
+        logit = torch.where(seen, (q[..., f] @ K[..., f].transpose(-1, -2)) / math.sqrt(w), -math.inf)
+        size = torch.where(seen, (q[..., f].abs() @ K[..., f].abs().transpose(-1, -2)) / math.sqrt(w), 0.0).amax(-1, keepdim=True)
+        e = torch.exp(logit - logit.amax(-1, keepdim=True))
+        total = e.sum(-1, keepdim=True)
+        tau = 2.0 ** -11 + EPS32 * (2 * (m_c + m_d) + 4 * (w + 16) * (size + 1))
+        maps.append(((e / total) @ V, (tau * (e @ V.abs()) + 2.0 ** -35 * (seen.double() @ V.abs())) / total))
+    y, err = maps[0]
+    if x.maps == 2:
+        l = lam.double().view(g, p, 1, 1)
+        y, err = y - l * maps[1][0], err + l.abs() * maps[1][1] + 4 * EPS32 * (y.abs() + (l * maps[1][0]).abs())
+    return y.reshape(b, h, n, d), (HALF_BF16 * y.abs() + (1 + HALF_BF16) * err + 1e-30).reshape(b, h, n, d)
+
+
+def within(x, lam=None):
+    with x.plan() as plan:
+        assert plan.info()["ctx_kernel"] == 2  # the many-row kernel
+        got = attend(x, plan, lam=lam)
+    ref, tol = bounds(x, lam)
+    over = ((got - ref).abs() / tol).max().item()
+    print(f"largest error {over:.3f} of the tolerance", flush=True)
+    assert over <= 1
+
+
+def put(x, K=None, V=None):
+    """Store the changed rows {"ctx": [g, rows, d], "own": [b, g, rows, d]}."""
+    for name, rows, scale in (("K", K, x.k_scale), ("V", V, x.v_scale)):
+        if rows is not None:
+            x.ctx[name] = x._put(name, rows["ctx"][None], x.ctx_table.view(1, -1), torch.tensor([x.m_c]), scale)[0]
+            x.own[name] = x._put(name, rows["own"], x.tables, x.lens, scale)
+
+
+MANY = [
+    # b, h, g, d, m_c, m_d, n, page, maps
+    (5, 32, 4, 128, 700, 20, 2, 16, 1),                       # 80 rows per group: four-wave work-groups
+    (40, 32, 4, 128, 1500, 20, 1, 64, 1),                     # 320
+    (9, 16, 4, 128, 700, 33, 1, 16, 2),
+    (70, 16, 4, 64, 900, 20, 1, 32, 2),
+]
+IDS = ["many4", "many8", "diff4", "diff8"]
+
+
+@pytest.mark.parametrize("logit", [-45, 14, 16, 18, 21])
+@pytest.mark.parametrize("kv", ["fp8_e4m3", "mxfp4"])
+@pytest.mark.parametrize("case", MANY, ids=IDS)
+def test_context_weights_beside_a_dominant_key(case, kv, logit):
+    """The first context key has a logit far from all others and a value row of
+    zeros (an attention sink): the output comes from the others' small weights."""
+    *dims, maps = case
+    x = Problem(*dims, kv, maps=maps, seed=50)
+    w = x.d // maps
+    K = {"ctx": x.ctx["K"].clone(), "own": x.own["K"].clone()}
+    V = {"ctx": x.ctx["V"].clone(), "own": x.own["V"].clone()}
+    K["ctx"][:, 0], V["ctx"][:, 0] = 0, 0
+    for u in range(maps):
+        x.q[..., u * w] = 64
+        K["ctx"][:, 1:, u * w], K["own"][..., u * w] = 0, 0
+        K["ctx"][:, 0, u * w] = logit * math.sqrt(w) / 64
+    put(x, K, V)
+    within(x, lam=torch.linspace(-0.2, 0.9, x.h))
+
+
+@pytest.mark.parametrize("kv", ["fp8_e4m3", "mxfp4"])
+@pytest.mark.parametrize("case", MANY, ids=IDS)
+def test_rising_logits_over_codes(case, kv):
+    *dims, maps = case
+    x = Problem(*dims, kv, maps=maps, seed=51)
+    x.q = x.q.abs()
+    ramp = {name: torch.linspace(0.05, 2, rows).double().view(-1, 1) for name, rows in (("ctx", x.m_c), ("own", x.m_d))}
+    put(x, {name: getattr(x, name)["K"].abs() * ramp[name] for name in ramp})
+    within(x, lam=torch.linspace(-0.2, 0.9, x.h))
