@@ -458,7 +458,7 @@ bifattn_status_t bifattn_paged_gather(bifattn_paged_plan_t plan, const bifattn_p
  * shape, rounded once. The weights enter the value product with 15 bits; where
  * many query rows share a context of codes, with 11, below 2^-24 of the row's
  * largest weight among the keys of one work-group in fixed steps of 2^-34 of it,
- * and MXFP4 values of one column of 32 elements then count down to 2^-31 of the
+ * and MXFP4 values of one column of 32 elements then count down to 2^-36 of the
  * largest scale in it.
  * Infinities and NaN reach the tokens that see their row, and no other.
  * ctx_table [ceil(m_c / page)], tables [b][ceil(m_d_max / page)]; ctx_table may

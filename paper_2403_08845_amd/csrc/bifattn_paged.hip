@@ -686,8 +686,9 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
 // 58 and 37.4 with 5, 182, 60 and 38.0 with 4, 193, 66 and 43.6 with 2. E4M3 values
 // are exact in fp16. MXFP4
 // values enter relative to the largest scale of the same 32 elements among the
-// work-group's keys, read ahead (1/16 of the chunk's value bytes), and are exact
-// down to 2^-31 of it.
+// work-group's keys, read ahead (1/16 of the chunk's value bytes), which enters as
+// 2^13 (the largest value is then 6 * 2^13 of fp16's 65504), and are exact down to
+// 2^-36 of it.
 template <int D, int NW, int SK, typename KV, int MAPS>
 __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigned char* lds) {
   constexpr int KD = D / MAPS;             // dims of the logits
@@ -784,7 +785,7 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   stage_get(0);
   if (SK < nkeys) get_ids(SK);
   if constexpr (KV::MX) {
-    // the largest scale byte of each column that is a number; values then reach 6 * 2^8
+    // the largest scale byte of each column that is a number; values then reach 6 * 2^13
     static_assert(CPR == EB && (64 * NW) % EB == 0, "a chunk is a scale block, a thread's column stays");
     int top[EB];
 #pragma unroll
@@ -806,7 +807,7 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
     for (int c = 0; c < EB; ++c) {
 #pragma unroll
       for (int w = 0; w < NW; ++w) top[c] = max(top[c], tops[w * EB + c]);
-      vrefs[c] = __builtin_amdgcn_readfirstlane(top[c]) - 127 - 8;
+      vrefs[c] = __builtin_amdgcn_readfirstlane(top[c]) - 127 - 13;
       vref = (int)threadIdx.x % EB == c ? vrefs[c] : vref;
     }
     __syncthreads();

@@ -108,3 +108,21 @@ def test_rising_logits_over_codes(case, kv):
     ramp = {name: torch.linspace(0.05, 2, rows).double().view(-1, 1) for name, rows in (("ctx", x.m_c), ("own", x.m_d))}
     put(x, {name: getattr(x, name)["K"].abs() * ramp[name] for name in ramp})
     within(x, lam=torch.linspace(-0.2, 0.9, x.h))
+
+
+@pytest.mark.parametrize("case", MANY, ids=IDS)
+def test_values_beside_a_far_larger_one_of_their_column(case):
+    """MXFP4 values 2^-34 times the largest of their column, whose key has next to
+    no weight."""
+    *dims, maps = case
+    x = Problem(*dims, "mxfp4", maps=maps, seed=52)
+    w = x.d // maps
+    K = {"ctx": x.ctx["K"].clone(), "own": x.own["K"].clone()}
+    V = {"ctx": x.ctx["V"] * 2.0 ** -34, "own": x.own["V"] * 2.0 ** -34}
+    K["ctx"][:, 0], V["ctx"][:, 0] = 0, 6
+    for u in range(maps):
+        x.q[..., u * w] = 64
+        K["ctx"][:, 1:, u * w], K["own"][..., u * w] = 0, 0
+        K["ctx"][:, 0, u * w] = -64 * math.sqrt(w) / 64
+    put(x, K, V)
+    within(x, lam=torch.linspace(-0.2, 0.9, x.h))
