@@ -254,7 +254,7 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
 }
 
 // Read-out: a thread's 8 elements of a row, widened (times the group's scale)
-// to bf16. Rows at or past a sample's length are not written. Bytes alone: 8192
+// to bf16, rounded once. Rows at or past a sample's length are not written. Bytes alone: 8192
 // rows of 8 heads from MXFP4 9.3 us for 43 MB, 4.6 TB/s.
 template <int D, int KV>
 __global__ __launch_bounds__(256) void gather_kernel(PagedGatherParams P) {
@@ -289,13 +289,27 @@ __global__ __launch_bounds__(256) void gather_kernel(PagedGatherParams P) {
         const float* sc = u ? P.pool.v_scale : P.pool.k_scale;
         const float s = sc ? sc[gam] : 1.f;
         if (c == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(P.status, kStatusScale);
+        // Code times scale has 28 bits. Rounded to fp32 first, it goes to another bf16
+        // value than at once only where it meets the middle between two: then (1 in
+        // 2^16) formed in 64 bits and rounded to odd.
+        float f[8], p[8];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)b[e], false);
           const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)b[e], true);
-          w[2 * e] = pack_bf16(lo[0] * s, lo[1] * s);
-          w[2 * e + 1] = pack_bf16(hi[0] * s, hi[1] * s);
+          f[4 * e] = lo[0], f[4 * e + 1] = lo[1], f[4 * e + 2] = hi[0], f[4 * e + 3] = hi[1];
         }
+        uint32_t off = 0xffffu;  // 0: a product in the middle
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = f[e] * s;
+          off = min(off, (__float_as_uint(p[e]) & 0xffffu) ^ 0x8000u);
+        }
+        if (off == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = odd_f32((double)f[e] * (double)s);
+        }
+        w = to_bf16(p);
       } else {
         const uint32_t b = *reinterpret_cast<const uint32_t*>(src + 4 * c);
         const float s = __uint_as_float((uint32_t)((u ? P.pool.V_exp : P.pool.K_exp) + at * EB)[c / 4] << 23);

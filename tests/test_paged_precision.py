@@ -126,3 +126,39 @@ def test_values_beside_a_far_larger_one_of_their_column(case):
         K["ctx"][:, 0, u * w] = -64 * math.sqrt(w) / 64
     put(x, K, V)
     within(x, lam=torch.linspace(-0.2, 0.9, x.h))
+
+
+def test_fp8_read_out_is_rounded_once():
+    """Products of a code and a scale just off the middle between two bf16 values:
+    rounded to fp32 first they would meet it and go to the even one."""
+    codes = torch.arange(256, dtype=torch.uint8)
+    codes = codes[(codes & 127) != 127]
+    values = codes.view(torch.float8_e4m3fn).double()
+    r = torch.Generator().manual_seed(1)
+    scale = torch.exp2(8 * torch.rand(1 << 16, generator=r) - 4)
+    exact = values * scale.double().view(-1, 1)  # 28 bits
+
+    def nearest(y):  # bf16, in one rounding
+        step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -126))) - 7)
+        return torch.round(y / step) * step
+
+    twice = exact.float().to(torch.bfloat16).double()
+    bad = (nearest(exact) != twice).any(1).nonzero().flatten()
+    assert bad.numel() >= 2
+    g, rows = 16, 4
+    scale = torch.cat((scale[bad], scale))[:g].contiguous()
+    x = Problem(1, g, g, 64, 0, rows, page=16, kv="fp8_e4m3", lens=[rows], seed=8)
+    x.k_scale, x.v_scale = scale, scale.flip(0).contiguous()
+    page = int(x.tables[0, 0])
+    stored = torch.zeros(rows * 64, dtype=torch.uint8)
+    stored[:codes.numel()] = codes
+    stored = stored.view(rows, 64)
+    for name in "KV":
+        x.pool[name][page, :, :rows] = stored
+    outs = [torch.zeros(1, g, rows, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    with x.plan() as plan:
+        bif.bifattn_paged_gather(plan, x.pages(), x.tables.cuda(), x.lens.cuda(), *outs)
+        assert bif.bifattn_paged_plan_status(plan) == bif.OK
+    for got, s in zip(outs, (x.k_scale, x.v_scale)):
+        want = nearest(stored.view(torch.float8_e4m3fn).double() * s.double().view(-1, 1, 1))
+        assert torch.equal(got[0].cpu().double(), want)
