@@ -47,14 +47,24 @@ __device__ __forceinline__ void rotate(float& x, float& y, const Turn& a) {
   y = __builtin_fmaf(x, a[2], y * a[0]) + finite_rest(__builtin_fmaf(x, a[3], y * a[1]));
   x = p;
 }
-// The same in 64 bits, times f and rounded to odd, for codes: an element next
+// The same in 64 bits, scaled and rounded to odd, for codes: an element next
 // to a border between two codes falls on its side.
-__device__ __forceinline__ void rotate_odd(float& x, float& y, const Turn& a, double f) {
+template <typename S> __device__ __forceinline__ void rotate_odd(float& x, float& y, const Turn& a, const S& scaled) {
   const double c = (double)a[0] + (double)a[1], s = (double)a[2] + (double)a[3];
   const double u = x, v = y;
-  x = odd_f32((u * c - v * s) * f);
-  y = odd_f32((u * s + v * c) * f);
+  x = odd_f32(scaled(u * c - v * s));
+  y = odd_f32(scaled(u * s + v * c));
 }
+// x / scale, correctly rounded: the product with the rounded reciprocal alone may
+// miss a quotient in the middle between two codes (147 / 49 is 3). Infinities and
+// quotients past the codes' range keep the product.
+struct OverScale {
+  double scale, inv;
+  __device__ __forceinline__ double operator()(double x) const {
+    const double q = x * inv;
+    return fabs(q) < 1e6 ? __builtin_fma(__builtin_fma(-q, scale, x), inv, q) : q;
+  }
+};
 // Two chunks of 8 whose elements rotate with `turn`: with each other, or in
 // neighbouring pairs.
 template <typename F>
@@ -221,18 +231,19 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
       const float* sc = is_k ? A.pool.k_scale : A.pool.v_scale;
       const float s = sc ? sc[gam] : 1.f;
       if (t == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(A.status, kStatusScale);
-      const double inv = 1.0 / (double)s;
+      const OverScale over = {(double)s, 1.0 / (double)s};
       if (rotates) {
-        rotate_chunks(fx, fy, angles, A.neighbours, [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, inv); });
+        rotate_chunks(fx, fy, angles, A.neighbours, [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, over); });
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) fx[e] = odd_f32(fx[e] * inv), fy[e] = odd_f32(fy[e] * inv);
+        for (int e = 0; e < 8; ++e) fx[e] = odd_f32(over(fx[e])), fy[e] = odd_f32(over(fy[e]));
       }
       *reinterpret_cast<u32x2*>(dst + 8 * c0) = to_fp8(fx);
       *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(fy);
     } else {
       if (rotates)
-        rotate_chunks(fx, fy, angles, A.neighbours, [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, 1.0); });
+        rotate_chunks(fx, fy, angles, A.neighbours,
+                      [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, [](double v) { return v; }); });
       // A block is four chunks, of several of the row's threads: their
       // exponents meet in LDS. A row's threads are neighbours in one wave,
       // whose LDS accesses execute in order.

@@ -162,3 +162,24 @@ def test_fp8_read_out_is_rounded_once():
     for got, s in zip(outs, (x.k_scale, x.v_scale)):
         want = nearest(stored.view(torch.float8_e4m3fn).double() * s.double().view(-1, 1, 1))
         assert torch.equal(got[0].cpu().double(), want)
+
+
+@pytest.mark.parametrize("rot", [0, 64])
+def test_fp8_ties_of_quotients(rot):
+    """x / scale exactly in the middle between two codes goes to the even one, also
+    where x times the rounded reciprocal of the scale is below it (147 / 49)."""
+    assert 147.0 * (1.0 / 49.0) < 3.0
+    x = Problem(1, 1, 1, 64, 0, 1, page=16, kv="fp8_e4m3", lens=[1], seed=9)
+    x.k_scale = x.v_scale = torch.tensor([49.0 / 64])
+    row = torch.zeros(64)
+    row[:4] = torch.tensor([147.0, -147.0, 49.0, 245.0]) * 2.0 ** -16  # 3, -3, 1 and 5 halves of the least code
+    kv = row.to(torch.bfloat16).view(1, 1, 1, 64).cuda()
+    pages = x.pages()
+    lens = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with x.plan() as plan:  # position 0: no turn
+        bif.bifattn_paged_append(plan, pages, x.tables.cuda(), lens, kv, kv, lens,
+                                 freqs=torch.ones(32, device="cuda") if rot else None)
+        assert bif.bifattn_paged_plan_status(plan) == bif.OK
+    for t in (pages.K, pages.V):
+        got = t[int(x.tables[0, 0]), 0, 0].cpu().view(torch.float8_e4m3fn).double()
+        assert got[:5].tolist() == [2 * 2.0 ** -9, -2 * 2.0 ** -9, 0, 2 * 2.0 ** -9, 0]
