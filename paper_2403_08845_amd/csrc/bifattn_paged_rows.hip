@@ -30,8 +30,9 @@ __device__ __forceinline__ u32x4 to_bf16(const float* f) {
 }
 
 // cos and sin of an angle, each as a part of 16 significant bits and the rest
-// (about 40 bits together): ch, cl, sh, sl.
+// (about 40 bits together): ch, cl, sh, sl; and in 64 bits.
 typedef f32x4 Turn;
+typedef double FullTurn __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void two_parts(double v, float& hi, float& lo) {
   hi = __uint_as_float(__float_as_uint((float)v) & 0xffffff00u);
   lo = (float)(v - (double)hi);
@@ -48,12 +49,12 @@ __device__ __forceinline__ void rotate(float& x, float& y, const Turn& a) {
   x = p;
 }
 // The same in 64 bits, scaled and rounded to odd, for codes: an element next
-// to a border between two codes falls on its side.
-template <typename S> __device__ __forceinline__ void rotate_odd(float& x, float& y, const Turn& a, const S& scaled) {
-  const double c = (double)a[0] + (double)a[1], s = (double)a[2] + (double)a[3];
+// to a border between two codes falls on its side, where it is 2^-50 of |x| + |y| or
+// more away from it.
+template <typename S> __device__ __forceinline__ void rotate_odd(float& x, float& y, const FullTurn& a, const S& scaled) {
   const double u = x, v = y;
-  x = odd_f32(scaled(u * c - v * s));
-  y = odd_f32(scaled(u * s + v * c));
+  x = odd_f32(scaled(u * a[0] - v * a[1]));
+  y = odd_f32(scaled(u * a[1] + v * a[0]));
 }
 // x / scale, correctly rounded: the product with the rounded reciprocal alone may
 // miss a quotient in the middle between two codes (147 / 49 is 3). Infinities and
@@ -67,8 +68,8 @@ struct OverScale {
 };
 // Two chunks of 8 whose elements rotate with `turn`: with each other, or in
 // neighbouring pairs.
-template <typename F>
-__device__ __forceinline__ void rotate_chunks(float* x, float* y, const Turn* a, bool neighbours, F&& turn) {
+template <typename T, typename F>
+__device__ __forceinline__ void rotate_chunks(float* x, float* y, const T* a, bool neighbours, F&& turn) {
   if (neighbours) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -146,6 +147,7 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
   constexpr int RB = paged_row_bytes(D, KV), EB = D / kMxBlock;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
   Turn* turn = reinterpret_cast<Turn*>(dyn);  // [tokens_per_block][rot/2]
+  FullTurn* full = reinterpret_cast<FullTurn*>(dyn) + A.tokens_per_block * (A.rot / 2);  // the same, for codes
   __shared__ int tops[ROWS][D / 8];
   const int per = A.token_blocks * A.head_blocks;
   const int i = blockIdx.x / per, in = blockIdx.x - i * per;
@@ -168,6 +170,7 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
     two_parts(c, ch, cl);
     two_parts(s, sh, sl);
     turn[k] = Turn{ch, cl, sh, sl};
+    if constexpr (KV != kPagedBf16) full[k] = FullTurn{c, s};
   }
   __syncthreads();  // also: every thread has read lens
   if (threadIdx.x == 0) {
@@ -202,12 +205,12 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
     const int64_t* st = is_q ? A.qs : (is_k ? A.ks : A.vs);
     const uint16_t* src = (is_q ? A.q : (is_k ? A.k : A.v)) + (int64_t)i * st[0] + (is_q ? head : gam) * st[1] + token * st[2];
     const u32x4 rx = load16(src + 8 * c0), ry = load16(src + 8 * c1);
-    const Turn* angles = turn + r * half + 8 * u;
+    const int first = r * half + 8 * u;  // of the pairs' angles
     float fx[8], fy[8];
     widen8(rx, fx);
     widen8(ry, fy);
     if (is_q) {
-      if (turns) rotate_chunks(fx, fy, angles, A.neighbours, rotate);
+      if (turns) rotate_chunks(fx, fy, turn + first, A.neighbours, rotate);
       uint16_t* dst = A.q_out + (((size_t)i * A.h + head) * A.n + token) * D;
       *reinterpret_cast<u32x4*>(dst + 8 * c0) = to_bf16(fx);
       *reinterpret_cast<u32x4*>(dst + 8 * c1) = to_bf16(fy);
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
     uint8_t* dst = (is_k ? A.pool.K : A.pool.V) + at * RB;
     const bool rotates = is_k && turns;
     if constexpr (KV == kPagedBf16) {
-      if (rotates) rotate_chunks(fx, fy, angles, A.neighbours, rotate);
+      if (rotates) rotate_chunks(fx, fy, turn + first, A.neighbours, rotate);
       *reinterpret_cast<u32x4*>(dst + 16 * c0) = to_bf16(fx);
       *reinterpret_cast<u32x4*>(dst + 16 * c1) = to_bf16(fy);
     } else if constexpr (KV == kPagedFp8) {
@@ -233,7 +236,8 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
       if (t == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(A.status, kStatusScale);
       const OverScale over = {(double)s, 1.0 / (double)s};
       if (rotates) {
-        rotate_chunks(fx, fy, angles, A.neighbours, [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, over); });
+        rotate_chunks(fx, fy, full + first, A.neighbours,
+                      [&](float& x, float& y, const FullTurn& a) { rotate_odd(x, y, a, over); });
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) fx[e] = odd_f32(over(fx[e])), fy[e] = odd_f32(over(fy[e]));
@@ -242,8 +246,8 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
       *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(fy);
     } else {
       if (rotates)
-        rotate_chunks(fx, fy, angles, A.neighbours,
-                      [&](float& x, float& y, const Turn& a) { rotate_odd(x, y, a, [](double v) { return v; }); });
+        rotate_chunks(fx, fy, full + first, A.neighbours,
+                      [&](float& x, float& y, const FullTurn& a) { rotate_odd(x, y, a, [](double v) { return v; }); });
       // A block is four chunks, of several of the row's threads: their
       // exponents meet in LDS. A row's threads are neighbours in one wave,
       // whose LDS accesses execute in order.
@@ -347,7 +351,7 @@ hipError_t go(void (*kernel)(Prm), int grid, int block, int lds, hipStream_t str
 
 hipError_t launch_paged_append(const PagedAppendParams& A, int kv, hipStream_t s, hipEvent_t stop) {
   const int grid = A.samples * A.token_blocks * A.head_blocks;
-  const int lds = A.tokens_per_block * (A.rot / 2) * (int)sizeof(Turn);
+  const int lds = A.tokens_per_block * (A.rot / 2) * (int)(sizeof(Turn) + (kv == kPagedBf16 ? 0 : sizeof(FullTurn)));
   auto run = [&](auto kernel) { return go(kernel, grid, kAppendThreads, lds, s, stop, A); };
   if (A.d == 128) {
     if (kv == kPagedBf16) return run(append_kernel<128, kPagedBf16>);

@@ -183,3 +183,43 @@ def test_fp8_ties_of_quotients(rot):
     for t in (pages.K, pages.V):
         got = t[int(x.tables[0, 0]), 0, 0].cpu().view(torch.float8_e4m3fn).double()
         assert got[:5].tolist() == [2 * 2.0 ** -9, -2 * 2.0 ** -9, 0, 2 * 2.0 ** -9, 0]
+
+
+# position, x, y, frequency near atan(x / y) / position: x cos - y sin cancels to
+# about 2^-25 and lies within 2^-14 of a border between E2M1 codes of unit 2^-26
+CANCELLED = [
+    (1, 1.5703125, 1.984375, 0.6694372296333313),
+    (4, 1.5703125, 1.984375, 0.16735930740833282),
+    (7, 1.3203125, 1.1484375, 0.12212946265935898),
+    (11, 1.7265625, 1.1328125, 0.09001261740922928),
+    (27, 1.7265625, 1.7265625, 0.0290888212621212),
+    (33, 1.578125, 1.1796875, 0.028147917240858078),
+    (37, 1.015625, 1.9140625, 0.01318476814776659),
+]
+
+
+@pytest.mark.parametrize("case", CANCELLED, ids=lambda c: "position%d" % c[0])
+def test_codes_of_cancelled_rotations(case):
+    """Cosine and sine enter codes with 64 bits: the element falls on its side of
+    the border (80-bit reference)."""
+    position, a, c, f = case
+    turn = np.longdouble(np.float32(f)) * position
+    z = float(np.abs(np.longdouble(a) * np.cos(turn) - np.longdouble(c) * np.sin(turn)) * np.longdouble(2) ** 26)
+    grid = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+    middle = (grid[1:] + grid[:-1]) / 2
+    assert 2.0 ** -20 < np.abs(z - middle).min() < 2.0 ** -14
+    want = int(np.searchsorted(middle, z))
+    x = Problem(1, 1, 1, 64, 0, 64, page=64, kv="mxfp4", lens=[64], seed=9)
+    row, freqs = torch.zeros(64), torch.zeros(32)
+    row[0] = 5 * 2.0 ** -26  # the largest of the block: unit 2^-26
+    row[1], row[33], freqs[1] = a, c, f
+    kv = row.to(torch.bfloat16).view(1, 1, 1, 64).cuda()
+    assert torch.equal(kv.cpu().float().flatten(), row)
+    pages = x.pages()
+    lens = torch.tensor([position], dtype=torch.int32, device="cuda")
+    with x.plan() as plan:
+        bif.bifattn_paged_append(plan, pages, x.tables.cuda(), lens, kv, kv, lens, freqs=freqs.cuda())
+        assert bif.bifattn_paged_plan_status(plan) == bif.OK
+    at = int(x.tables[0, 0]), 0, position
+    assert int(pages.K_exp[at][0]) == 127 - 26
+    assert int(pages.K[at][0]) >> 4 & 7 == want
