@@ -418,9 +418,10 @@ typedef struct {
  * Append: token r < counts[i] of sequence i becomes its row lens[i] + r.
  *   angle_j = position * freqs[j], position = row (context) or m_c + row (own)
  *   (x, y) -> (x cos - y sin, x sin + y cos) for each pair of q and k; v is not rotated
- * The angle is formed in 64 bits, at any position, and every element is rounded
- * once: q_out and bf16 rows to bf16 (from values off by 2^-22 of themselves),
- * codes from 64 bits: fp8 from x / scale, saturated at +-448; an MXFP4 block of 32 elements to the
+ * The angle is formed in 64 bits (off by 2^-51 of itself) and every element is
+ * rounded once: q_out and bf16 rows to bf16 (from values off by 2^-22 of
+ * themselves and 2^-37 of |x| + |y|), codes from 64 bits (off by 2^-50 of |x| +
+ * |y|): fp8 from x / scale, saturated at +-448; an MXFP4 block of 32 elements to the
  * scale 2^(floor(log2(largest)) - 2) (exponent within [-126, 127]) and the
  * nearest E2M1 values, ties to even, saturated at 6; a block that holds an
  * infinity or a NaN becomes NaN. q may overlap nothing that is written.

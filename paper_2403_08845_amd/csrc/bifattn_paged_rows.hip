@@ -39,9 +39,11 @@ __device__ __forceinline__ void two_parts(double v, float& hi, float& lo) {
 }
 // (x cos - y sin, x sin + y cos) of bf16 values. x * ch and y * sh have at most
 // 24 bits, so y * sh is exact and the fused product rounds the exact main part
-// once: the result is off by 2^-22 of itself, also where the terms cancel. The
-// rest of an infinite element has no meaning; it is kept finite (a finite
-// element's is below 2^113), so that the main part decides.
+// once: the result is off by 2^-22 of itself and, which shows where the terms
+// cancel, by 2^-37 of |x| + |y|: the rest (2^-15 of the terms) is cut and formed
+// with 24 bits, and the main part may exceed the result by as much. The rest of
+// an infinite element has no meaning; it is kept finite (a finite element's is
+// below 2^113), so that the main part decides.
 __device__ __forceinline__ float finite_rest(float r) { return __builtin_amdgcn_fmed3f(r, -0x1p120f, 0x1p120f); }
 __device__ __forceinline__ void rotate(float& x, float& y, const Turn& a) {
   const float p = __builtin_fmaf(x, a[0], -(y * a[2])) + finite_rest(__builtin_fmaf(x, a[1], -(y * a[3])));
@@ -130,11 +132,11 @@ __device__ __forceinline__ void widen8(const u32x4& r, float* f) {
 // h query rows, g key rows and g value rows of each. A row is d/16 threads'
 // work, each two chunks of 8 elements that rotate with each other.
 //
-// The angle of a pair is position * freq in 64 bits (positions reach 2^31 and
-// an fp32 product is off by 2^-24 of a turn per turn: 0.06 of a radian at 10^6),
-// formed once per token and pair and kept in LDS. Rotated queries and bf16 keys
-// are off by 2^-22 of themselves before their one rounding, codes are formed
-// from 64 bits.
+// The angle of a pair is position * freq in 64 bits, off by 2^-51 of itself
+// (positions reach 2^30 and an fp32 product is off by 2^-24 of a turn per turn: 0.06
+// of a radian at 10^6), formed once per token and pair and kept in LDS. Rotated
+// queries and bf16 keys are off by 2^-22 of themselves and 2^-37 of |x| + |y| before
+// their one rounding, codes are formed from 64 bits.
 //
 // Byte work where the batch is large (8192 tokens of 32 + 8 heads into MXFP4:
 // 46 us for 177 MB, 3.8 TB/s, of which a copy takes 35); a step of some tokens is

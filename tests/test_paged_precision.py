@@ -223,3 +223,37 @@ def test_codes_of_cancelled_rotations(case):
     at = int(x.tables[0, 0]), 0, position
     assert int(pages.K_exp[at][0]) == 127 - 26
     assert int(pages.K[at][0]) >> 4 & 7 == want
+
+
+def test_rotations_that_cancel():
+    """Rotated queries and bf16 keys against 80 bits: off by 2^-37 of |x| + |y| (the
+    rest of cosine and sine, 2^-15 of them, its two products and the main part's
+    excess over the result by as much, each rounded to 24 bits: four times 2^-39),
+    by the angle's 2^-51 of itself times that, and by one rounding; also at
+    positions near 2^29."""
+    n = 32
+    r = np.random.default_rng(4)
+    for m_c in (0, 3, (1 << 29) - 100):
+        x = Problem(1, 2, 1, 64, 0, 64, page=64, lens=[64], seed=9)
+        x.m_c = m_c
+        lo, hi = ((1 + r.integers(0, 128, 32) / 128) for _ in range(2))
+        freqs = (np.arctan2(lo, hi) / max(1, m_c) if m_c < 100 else r.uniform(0.5, 1, 32)).astype(np.float32)
+        row = torch.tensor(np.concatenate((lo, hi))).to(torch.bfloat16)
+        kv = row.view(1, 1, 1, 64).expand(1, 1, n, 64).contiguous().cuda()
+        q = kv.expand(1, 2, n, 64)
+        pages = x.pages()
+        out = torch.zeros(1, 2, n, 64, dtype=torch.bfloat16, device="cuda")
+        lens = torch.zeros(1, dtype=torch.int32, device="cuda")
+        with x.plan() as plan:
+            bif.bifattn_paged_append(plan, pages, x.tables.cuda(), lens, kv, kv, lens, q=q, q_out=out,
+                                     freqs=torch.from_numpy(freqs).cuda())
+            assert bif.bifattn_paged_plan_status(plan) == bif.OK
+        keys = pages.K[int(x.tables[0, 0]), 0].cpu().double().numpy()
+        for t in range(n):
+            turn = freqs.astype(np.longdouble) * (m_c + t)
+            c, s = np.cos(turn), np.sin(turn)
+            want = np.concatenate((lo * c - hi * s, lo * s + hi * c)).astype(np.float64)
+            size = np.tile(lo + hi, 2)
+            tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -37 + 2.0 ** -51 * np.tile(turn.astype(np.float64), 2)) * size
+            for got in (out[0, 0, t].cpu().double().numpy(), out[0, 1, t].cpu().double().numpy(), keys[t]):
+                assert (np.abs(got - want) <= tol).all()
