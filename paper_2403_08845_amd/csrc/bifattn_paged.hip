@@ -1013,11 +1013,22 @@ __device__ __forceinline__ u32x2 finish_row(const PagedCombineParams& C, int j, 
   if constexpr (MAPS == 2) {
     r -= C.lambda[j / C.ntok] * y1;
     if (C.weight) {
-      float sq = r[0] * r[0] + r[1] * r[1] + r[2] * r[2] + r[3] * r[3];
-      if constexpr (D == 128) sq = xor16_sum(sq);
+      auto mean_square = [&]() {
+        float sq = r[0] * r[0] + r[1] * r[1] + r[2] * r[2] + r[3] * r[3];
+        if constexpr (D == 128) sq = xor16_sum(sq);
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
-      const float mean = sq * (1.f / D) + C.eps;  // 0: a row of zeros, which stays one
+        for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
+        return sq * (1.f / D);
+      };
+      float mean = mean_square() + C.eps;
+      // Squares at the ends of fp32's range, or past them: once more with the row
+      // times a power of two, which the quotient does not see.
+      const bool fits = mean > 0x1p-80f && mean < 0x1p120f;
+      if (__any(!fits)) {
+        const float by = fits ? 1.f : mean < 1.f ? 0x1p96f : 0x1p-70f;
+        r *= by;
+        mean = mean_square() + C.eps * by * by;  // 0: a row of zeros, which stays one
+      }
       r *= *reinterpret_cast<const f32x4*>(C.weight + col) * (mean == 0.f ? 0.f : 1.f / sqrtf(mean));
     }
     r *= C.out_scale;

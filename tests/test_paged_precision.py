@@ -257,3 +257,18 @@ def test_rotations_that_cancel():
             tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -37 + 2.0 ** -51 * np.tile(turn.astype(np.float64), 2)) * size
             for got in (out[0, 0, t].cpu().double().numpy(), out[0, 1, t].cpu().double().numpy(), keys[t]):
                 assert (np.abs(got - want) <= tol).all()
+
+
+@pytest.mark.parametrize("launches", ["parts", "one launch"])
+@pytest.mark.parametrize("power", [-95, -80, 64, 90])
+@pytest.mark.parametrize("d", [64, 128])
+def test_norm_of_tiny_and_huge_heads(d, power, launches, monkeypatch):
+    """Heads whose squares leave fp32's range are normalised like others."""
+    monkeypatch.setenv("BIFATTN_WHOLE", "2" if launches == "parts" else "1")
+    x = Problem(3, 8, 2, d, 40, 40, page=32, maps=2, lens=[0, 7, 40], seed=15)
+    put(x, V={name: getattr(x, name)["V"] * 2.0 ** power for name in ("ctx", "own")})
+    lam, weight = torch.full((x.h,), 0.5), torch.randn(x.d, generator=x.rng)
+    for eps in (0.0, 1e-5):
+        got = attend(x, lam=lam, weight=weight, eps=eps)
+        ref, tol = x.attention(lam=lam, weight=weight, eps=eps)
+        assert ((got - ref).abs() <= tol).all(), eps
