@@ -426,7 +426,9 @@ typedef struct {
  * nearest E2M1 values, ties to even, saturated at 6; a block that holds an
  * infinity or a NaN becomes NaN. q may overlap nothing that is written.
  *   lens_out[i] = lens[i] + counts[i]
- * lens_out may be lens (advanced in place); otherwise the two do not overlap.
+ * lens_out may be lens (advanced in place) or counts (replaced); where it
+ * overlaps a part of either, the call is refused (EINVAL). It overlaps nothing
+ * else that the call reads or writes.
  * Rows past the sequence's capacity
  * (m_c or m_d_max) are dropped, the length stops there, a length outside its
  * range is clamped first; all raise the ELENS flag. q_out rows of tokens past

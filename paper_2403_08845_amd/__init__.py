@@ -649,7 +649,7 @@ def bifattn_paged_append(plan: PagedPlan, pages: Pages, table, lens, k, v, lens_
     shared context, s = 1). With freqs (fp32 [rot/2]) keys and queries are
     rotated to their positions; q bf16 [s, h, n, d] goes to q_out, contiguous.
     k, v and q may be strided. lens_out int32 [s] receives the new lengths and
-    may be lens."""
+    may be lens or counts."""
     caller = getattr(plan, "_caller", None)
     if caller is not None and _taken(caller.append(pages, table, lens, k, v, lens_out, q, q_out, counts, freqs, neighbours, context,
                                             None if stream is None else _stream_ptr(stream).value or 0), "bifattn_paged_append"):

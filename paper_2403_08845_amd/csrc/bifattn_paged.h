@@ -90,8 +90,9 @@ struct PagedAppendParams {
   const int32_t* table;     // [samples][table_pages]
   const int32_t* lens;      // [samples] first row to write
   const int32_t* counts;    // [samples] new rows, or null for n
-  int32_t* lens_out;        // [samples]; may be lens
-  int* tickets;             // [samples], zero between calls: work-groups that have read lens
+  int32_t* lens_out;        // [samples]; may be lens or counts
+  int in_place;             // it is one of them
+  int* tickets;             // [samples], zero between calls: work-groups that have read lens and counts
   int* status;
   const uint16_t* q;        // null: no queries
   const uint16_t* k;

@@ -556,6 +556,16 @@ bifattn_status_t bifattn_paged_append(bifattn_paged_plan_t P, const bifattn_page
     A.ks[k] = rows->k_stride[k];
     A.vs[k] = rows->v_stride[k];
   }
+  // lens_out may be lens or counts, whose elements the kernel then replaces when
+  // all have been read; a part of one would be another sample's input.
+  for (const int32_t* in : {lens, rows->counts}) {
+    if (!in) continue;
+    const uintptr_t a = (uintptr_t)in, z = (uintptr_t)lens_out, bytes = 4 * (uintptr_t)rows->samples;
+    if (a == z)
+      A.in_place = 1;
+    else if (a < z + bytes && z < a + bytes)
+      return BIFATTN_EINVAL;
+  }
   A.table = table;
   A.lens = lens;
   A.counts = rows->counts;

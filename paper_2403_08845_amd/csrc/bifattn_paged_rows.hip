@@ -174,13 +174,13 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
     turn[k] = Turn{ch, cl, sh, sl};
     if constexpr (KV != kPagedBf16) full[k] = FullTurn{c, s};
   }
-  __syncthreads();  // also: every thread has read lens
+  __syncthreads();  // also: every thread has read lens and counts
   if (threadIdx.x == 0) {
-    if (A.lens_out != A.lens) {
+    if (!A.in_place) {
       if (in == 0) A.lens_out[i] = start + fit;
     } else if (per == 1) {
       A.lens_out[i] = start + fit;
-    } else if (atomicAdd(A.tickets + i, 1) == per - 1) {  // the others have read the length
+    } else if (atomicAdd(A.tickets + i, 1) == per - 1) {  // the others have read theirs
       A.tickets[i] = 0;
       A.lens_out[i] = start + fit;
     }
