@@ -619,8 +619,10 @@ def _pages(plan, pages):
         _ptr_or_none(pages.v_scale, (D.g,), torch.float32, dev, "pages.v_scale")))
 
 
-def _table_shape(D, samples, context):
-    return (samples, -(-(D.m_c if context else D.m_d_max) // D.page))
+def _table_shapes(D, samples, context):
+    """[samples, pages], or [pages] too for the context's one sequence."""
+    pages = -(-(D.m_c if context else D.m_d_max) // D.page)
+    return [(pages,), (1, pages)] if context and samples == 1 else [(samples, pages)]
 
 
 def _rows(t, heads, samples, n, d, device, name):
@@ -646,7 +648,7 @@ def bifattn_paged_append(plan: PagedPlan, pages: Pages, table, lens, k, v, lens_
     """Enqueue the append of new tokens (see include/bifattn.h): k, v bf16
     [s, g, n, d] become rows lens[i] .. lens[i] + counts[i] - 1 (counts None:
     n each) of the s sequences that table int32 [s, pages] names (context: the
-    shared context, s = 1). With freqs (fp32 [rot/2]) keys and queries are
+    shared context, s = 1, whose table may be [pages] as in the attention calls). With freqs (fp32 [rot/2]) keys and queries are
     rotated to their positions; q bf16 [s, h, n, d] goes to q_out, contiguous.
     k, v and q may be strided. lens_out int32 [s] receives the new lengths and
     may be lens or counts."""
@@ -675,7 +677,7 @@ def bifattn_paged_append(plan: PagedPlan, pages: Pages, table, lens, k, v, lens_
                     _ptr_or_none(freqs, (half,), torch.float32, dev, "freqs"), qp, kp, vp, qs, ks, vs,
                     _ptr_or_none(q_out, (s, D.h, n, D.d), torch.bfloat16, dev, "q_out"))
     _check(lib().bifattn_paged_append(
-        plan.handle, _pages(plan, pages), _tensor(table, _table_shape(D, s, context), i32, dev, "table"),
+        plan.handle, _pages(plan, pages), _tensor(table, _table_shapes(D, s, context), i32, dev, "table"),
         ctypes.byref(rows), _tensor(lens, (s,), i32, dev, "lens"),
         _tensor(lens_out, (s,), i32, dev, "lens_out"), _stream_ptr(stream, dev)), "bifattn_paged_append")
 
@@ -683,7 +685,7 @@ def bifattn_paged_append(plan: PagedPlan, pages: Pages, table, lens, k, v, lens_
 def bifattn_paged_gather(plan: PagedPlan, pages: Pages, table, lens, k_out, v_out, *, first=None,
                          context=False, stream=None):
     """Enqueue the read-out of rows first[i] .. (first None: 0) of each sequence
-    as bf16 into k_out, v_out [s, g, rows, d]; rows at or past lens[i] are left
+    of the table (as in bifattn_paged_append) as bf16 into k_out, v_out [s, g, rows, d]; rows at or past lens[i] are left
     as they were."""
     caller = getattr(plan, "_caller", None)
     if caller is not None and _taken(caller.gather(pages, table, lens, k_out, v_out, first, context,
@@ -696,7 +698,7 @@ def bifattn_paged_gather(plan: PagedPlan, pages: Pages, table, lens, k_out, v_ou
     shape, i32 = (s, D.g, rows, D.d), torch.int32
     outs = [_tensor(t, shape, torch.bfloat16, dev, name) for t, name in ((k_out, "k_out"), (v_out, "v_out"))]
     _check(lib().bifattn_paged_gather(
-        plan.handle, _pages(plan, pages), _tensor(table, _table_shape(D, s, context), i32, dev, "table"),
+        plan.handle, _pages(plan, pages), _tensor(table, _table_shapes(D, s, context), i32, dev, "table"),
         _ptr_or_none(first, (s,), i32, dev, "first"), _tensor(lens, (s,), i32, dev, "lens"), s, rows,
         int(bool(context)), *outs, _stream_ptr(stream, dev)), "bifattn_paged_gather")
 
@@ -704,19 +706,18 @@ def bifattn_paged_gather(plan: PagedPlan, pages: Pages, table, lens, k_out, v_ou
 def _attention_args(plan, q, ctx_table, tables, lens, out):
     torch, D, dev = _torch(), plan.dims, plan.device
     i32 = torch.int32
-    ctx = [(_table_shape(D, 1, True)[1],), _table_shape(D, 1, True)]
     qp = _tensor(q, _query_shapes(D), torch.bfloat16, dev, "q")
-    return (qp, ctypes.c_void_p(None) if D.m_c == 0 else _tensor(ctx_table, ctx, i32, dev, "ctx_table"),
+    return (qp, ctypes.c_void_p(None) if D.m_c == 0 else _tensor(ctx_table, _table_shapes(D, 1, True), i32, dev, "ctx_table"),
             ctypes.c_void_p(None) if D.m_d_max == 0 else
-            _tensor(tables, _table_shape(D, D.b, False), i32, dev, "tables"),
+            _tensor(tables, _table_shapes(D, D.b, False), i32, dev, "tables"),
             ctypes.c_void_p(None) if D.m_d_max == 0 else _tensor(lens, (D.b,), i32, dev, "lens"),
             _tensor(out, [tuple(q.shape)], torch.bfloat16, dev, "out"))
 
 
 def bifattn_paged_decode(plan: PagedPlan, q, pages: Pages, ctx_table, tables, lens, out, stream=None):
     """Enqueue one decode-attention step over the pages (see include/bifattn.h):
-    q bf16 [b,h,n,d] ([b,h,d] when n = 1), ctx_table int32 [pages] of the shared
-    context, tables int32 [b, pages] and lens int32 [b] of the own rows; out
+    q bf16 [b,h,n,d] ([b,h,d] when n = 1), ctx_table int32 [pages] (or [1, pages]) of
+    the shared context, tables int32 [b, pages] and lens int32 [b] of the own rows; out
     bf16 shaped like q."""
     caller = getattr(plan, "_caller", None)
     if caller is not None and _taken(caller.decode(q, pages, ctx_table, tables, lens, out,

@@ -272,6 +272,13 @@ int64_t pages_of(const PagedCaller* P, bool context) {
   return (rows + P->page - 1) / P->page;
 }
 
+// A table of page ids: [samples, pages], or [pages] too for the context's one sequence.
+bool take_table(PyObject* o, const PagedCaller* P, int64_t samples, bool context, void** ptr) {
+  const int64_t pages = pages_of(P, context);
+  return (context && samples == 1 && take(o, &P->base, at::kInt, {pages}, ptr)) ||
+         take(o, &P->base, at::kInt, {samples, pages}, ptr);
+}
+
 // The tensors that both attention calls take: q, pages, ctx_table, tables, lens, out.
 struct AttentionArgs {
   void *q, *out, *ctx = nullptr, *tables = nullptr, *lens = nullptr;
@@ -289,8 +296,8 @@ bool take_attention(PyObject* const* a, PyObject* out, const PagedCaller* P, Att
     return false;
   }
   if (!take_pages(a[1], P, &r->pages)) return false;
-  if (C->m_c > 0 && !take(a[2], C, at::kInt, {pages_of(P, true)}, &r->ctx)) return false;
-  return C->m_d == 0 || (take(a[3], C, at::kInt, {C->b, pages_of(P, false)}, &r->tables) &&
+  if (C->m_c > 0 && !take_table(a[2], P, 1, true, &r->ctx)) return false;
+  return C->m_d == 0 || (take_table(a[3], P, C->b, false, &r->tables) &&
                          take(a[4], C, at::kInt, {C->b}, &r->lens));
 }
 
@@ -394,7 +401,7 @@ PyObject* paged_append(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
       r.freqs = static_cast<const float*>(p);
       r.rot = (int32_t)(2 * f->size(0));
     }
-    if (!take_pages(a[0], P, &pages) || !take(a[1], C, at::kInt, {s, pages_of(P, r.context)}, &table) ||
+    if (!take_pages(a[0], P, &pages) || !take_table(a[1], P, s, r.context, &table) ||
         !take(a[2], C, at::kInt, {s}, &lens) || !take(a[5], C, at::kInt, {s}, &lens_out) ||
         !take_stream(a[12], C, &stream))
       Py_RETURN_NONE;
@@ -430,7 +437,7 @@ PyObject* paged_gather(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
     s = k->size(0), rows = k->size(2);
     if (!take(a[3], C, at::kBFloat16, {s, C->g, rows, C->d}, &k_out) ||
         !take(a[4], C, at::kBFloat16, {s, C->g, rows, C->d}, &v_out) || !take_pages(a[0], P, &pages) ||
-        !take(a[1], C, at::kInt, {s, pages_of(P, context)}, &table) || !take(a[2], C, at::kInt, {s}, &lens) ||
+        !take_table(a[1], P, s, context, &table) || !take(a[2], C, at::kInt, {s}, &lens) ||
         !optional(a[5], C, at::kInt, {s}, &first) || !take_stream(a[7], C, &stream))
       Py_RETURN_NONE;
   } catch (...) {
