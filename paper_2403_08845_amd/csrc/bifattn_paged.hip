@@ -297,11 +297,12 @@ __device__ __forceinline__ void take_odd_values(PageState<D, NT>& st, unsigned c
 }
 
 // One staged tile against NT query tiles. rem: keys from the tile's first to
-// the end of the sequence; row r sees keys < rem - (ntok - 1) + r % ntok.
+// the end of the sequence; row r sees keys < rem - (ntok - 1) + r % ntok. second:
+// the first row of the second map, 0 with one map.
 template <int D, int NT, typename KV, typename QAt>
 __device__ __forceinline__ void page_update(PageState<D, NT>& st, const PageTile<D, KV>& A,
                                             const unsigned char* kl, unsigned char* vl, QAt&& q_at,
-                                            int rem, int ntok, float scale_log2, int lane) {
+                                            int rem, int ntok, int second, float scale_log2, int lane) {
   constexpr int KS = D / 32, DV = D / 16;
   const int G = lane >> 4;
   f32x4 sacc[NT][2];
@@ -315,6 +316,35 @@ __device__ __forceinline__ void page_update(PageState<D, NT>& st, const PageTile
       const u32x4 qo = q_at(nt, s);
       sacc[nt][0] = mfma_bf16(k0, qo, sacc[nt][0]);
       sacc[nt][1] = mfma_bf16(k1, qo, sacc[nt][1]);
+    }
+  }
+  // An infinity in the other map's half of a key met the zeros of this map's row:
+  // where a logit is NaN, every row once more over its own half alone. (Codes have
+  // no infinities, and a NaN makes the maps' difference NaN through either.)
+  if constexpr (KV::BITS == 16) {
+    if (second) {
+      bool odd = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) odd |= sacc[nt][e / 4][e % 4] != sacc[nt][e / 4][e % 4];
+      if (__any(odd)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            f32x4 half[2];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+              f32x4& h = half[s / (KS / 2)];
+              if (s % (KS / 2) == 0) h = f32x4{0.f, 0.f, 0.f, 0.f};
+              h = mfma_bf16(A.kop(kl, a, s, lane), q_at(nt, s), h);
+            }
+            const bool upper = nt * kRowsPerTile + (lane & 15) >= second;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sacc[nt][a][j] = upper ? half[1][j] : half[0][j];
+          }
+      }
     }
   }
   // The reference maximum only has to bound the logits within 2^kRescaleSlack:
@@ -420,7 +450,7 @@ template <int D, int NT, typename KV, int AUX = kAuxStream, typename QAt>
 __device__ __forceinline__ bool stream_pages(PageState<D, NT>& st, const PagePool& P, int gam,
                                              const int32_t* table, QAt&& q_at, unsigned char* kl,
                                              unsigned char* vl, int ids0, int ids1, int k0, int k1, int kend,
-                                             int stride, int ntok, float scale_log2, int lane) {
+                                             int stride, int ntok, int second, float scale_log2, int lane) {
   constexpr int DEPTH = KV::BITS == 16 ? 1 : 2;
   bool bad = false;
   if (k0 >= k1) return false;
@@ -447,7 +477,7 @@ __device__ __forceinline__ bool stream_pages(PageState<D, NT>& st, const PagePoo
       const int ids = next;
       next = ids_at(key + (DEPTH + 1) * stride);
       load(T[u], ids, key + DEPTH * stride);
-      page_update(st, KV::MX ? cur : T[u], kl, vl, q_at, kend - key, ntok, scale_log2, lane);
+      page_update(st, KV::MX ? cur : T[u], kl, vl, q_at, kend - key, ntok, second, scale_log2, lane);
       key += stride;
       if (key >= k1) break;
     }
@@ -516,7 +546,7 @@ __device__ __forceinline__ void own_block(const PagedAttnParams& P, int blk, boo
   st.init();
   const bool bad =
       stream_pages<D, NT, KV>(st, P.pool, gam, table, q_at, kl, vl, ids0, ids1, k0, min(total, c0 + P.dec_keys), total,
-                              stride, P.ntok, group_scale_log2(P, gam), lane);
+                              stride, P.ntok, P.maps == 2 ? P.pn : 0, group_scale_log2(P, gam), lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
   const size_t prow = (((size_t)ig * P.S_d + s) * kWaves + wave) * P.R;
@@ -612,7 +642,7 @@ __device__ __forceinline__ void ctx_few_block(const PagedAttnParams& P, int blk,
   PageState<D, NT> st;
   st.init();
   const bool bad = stream_pages<D, NT, KV>(st, P.pool, gam, P.ctx_table, q_at, kl, vl, ids0, ids1, k0, P.m_c, P.m_c, stride,
-                                           1, group_scale_log2(P, gam), lane);
+                                           1, P.maps == 2 ? P.Mh : 0, group_scale_log2(P, gam), lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
   merge_states(st, merge, wave, lane);
@@ -1191,9 +1221,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const float sl2 = group_scale_log2(P, gam);
   // the context's rows are read by the group's other samples too: cached
   bool bad = stream_pages<D, NT, KV, 0>(st, P.pool, gam, P.ctx_table, q_at, kl, vl, c0, c1, k0, P.m_c, P.m_c, stride, 1,
-                                        sl2, lane);
+                                        MAPS == 2 ? P.pn : 0, sl2, lane);
   const int total = scalar(raw < 0 ? 0 : (raw > P.m_d_max ? P.m_d_max : raw));
-  bad |= stream_pages<D, NT, KV>(st, P.pool, gam, table, q_at, kl, vl, o0, o1, k0, total, total, stride, P.ntok, sl2, lane);
+  bad |= stream_pages<D, NT, KV>(st, P.pool, gam, table, q_at, kl, vl, o0, o1, k0, total, total, stride, P.ntok,
+                                     MAPS == 2 ? P.pn : 0, sl2, lane);
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   total_sums(st);
   float* merge = reinterpret_cast<float*>(lds + QB);

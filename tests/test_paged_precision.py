@@ -272,3 +272,29 @@ def test_norm_of_tiny_and_huge_heads(d, power, launches, monkeypatch):
         got = attend(x, lam=lam, weight=weight, eps=eps)
         ref, tol = x.attention(lam=lam, weight=weight, eps=eps)
         assert ((got - ref).abs() <= tol).all(), eps
+
+
+@pytest.mark.parametrize("launches", ["parts", "one launch"])
+@pytest.mark.parametrize("map_", [0, 1])
+@pytest.mark.parametrize("case", [(4, 4, 4, 128, 130, 16, 1, 16), (3, 8, 2, 64, 77, 40, 4, 32), (2, 16, 1, 128, 300, 33, 2, 64),
+                                  (9, 16, 4, 128, 515, 65, 1, 16)], ids=["few", "drafts", "four_tiles", "many"])
+def test_infinite_keys_of_one_map(case, map_, launches, monkeypatch):
+    """A key element of one map that is -infinity takes the key's weight in that
+    map alone, as a very negative finite one does."""
+    monkeypatch.setenv("BIFATTN_WHOLE", "2" if launches == "parts" else "1")
+    x = Problem(*case, "bf16", maps=2, lens=[case[5]] * case[0], seed=70)
+    at = map_ * x.d // 2 + 3
+    x.q[..., at] = 1
+    lam = torch.linspace(0.2, 0.9, x.h)
+    got = {}
+    for value in (-2.0 ** 60, -math.inf):
+        K = {name: getattr(x, name)["K"].clone() for name in ("ctx", "own")}
+        K["ctx"][:, 5, at], K["own"][:, :, 1, at] = value, value
+        put(x, K)
+        got[value] = attend(x, lam=lam)
+    assert torch.equal(got[-2.0 ** 60], got[-math.inf])
+    for rows in (x.ctx, x.own):  # a logit of -62 or less instead: next to no weight
+        rows["K"] = torch.where(rows["K"].isinf(), -500.0, rows["K"])
+    ref, tol = bounds(x, lam)
+    assert torch.isfinite(got[-math.inf]).all()
+    assert ((got[-math.inf] - ref).abs() <= tol).all()
