@@ -457,8 +457,9 @@ bifattn_status_t bifattn_paged_gather(bifattn_paged_plan_t plan, const bifattn_p
  * One decode-attention step over the pages (maps = 1):
  *   out[i, j, r, :] = softmax_t(scale * q[i,j,r,:] . K_i[t,:]) @ V_i
  * with K_i the context rows and own rows t < lens[i] - n + r + 1, V_i likewise;
- * 0 where a token sees no key at all, or none whose logit is above -infinity. q bf16 [b][h][n][d]; out bf16, the same
- * shape, rounded once. The weights enter the value product with 15 bits; where
+ * 0 where a token sees no key at all, or none whose logit is above -infinity. q
+ * bf16 [b][h][n][d]; out bf16, the same shape, rounded once. Finite logits count up
+ * to 2^25 in magnitude. The weights enter the value product with 15 bits; where
  * many query rows share a context of codes, with 11, below 2^-24 of the row's
  * largest weight among the keys of one work-group in fixed steps of 2^-34 of it,
  * and MXFP4 values of one column of 32 elements then count down to 2^-36 of the

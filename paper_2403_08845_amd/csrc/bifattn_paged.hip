@@ -704,21 +704,21 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
 //
 // Bound by what a block of 32 keys costs a CU: matrix cores, vector units and
 // LDS are each busy for about half of the cycles (256 samples of a grouped layer
-// over 32k rows in MXFP4: 176 us a step, 790 TFLOP/s). Code caches take fp16 for the
-// value product:
-// one term of 11 bits for the weights (their error 2e-4 beside the output's
-// 1.7e-3) where bf16 values need two. The weights enter 2^kUp times as large, so
-// that fp16's range lies where theirs does: with a slack of 2^5 above the reference
-// they keep 11 bits down to 2^-24 of the row's largest among the work-group's keys;
-// below, a fixed step of 2^-34 of it. A smaller slack reaches further and raises
-// more often: grouped layer over 32k in MXFP4, multi-query one over 16k in fp8 and
-// grouped differential one over 16k in MXFP4 in turn 180, 58 and 37.3 us with 8, 180.5,
-// 58 and 37.4 with 5, 182, 60 and 38.0 with 4, 193, 66 and 43.6 with 2. E4M3 values
-// are exact in fp16. MXFP4
-// values enter relative to the largest scale of the same 32 elements among the
-// work-group's keys, read ahead (1/16 of the chunk's value bytes), which enters as
-// 2^13 (the largest value is then 6 * 2^13 of fp16's 65504), and are exact down to
-// 2^-36 of it.
+// over 32k rows in MXFP4: 176 us a step, 790 TFLOP/s).
+//
+// Code caches take fp16 for the value product: one term of 11 bits for the weights
+// (their error 2e-4 beside the output's 1.7e-3) where bf16 values need two. The
+// reference lies 2^kUp below the largest weight, so that fp16's range lies where
+// theirs does: raised once a weight exceeds the last one's largest by 2^5, they keep
+// 11 bits down to 2^-24 of the row's largest among the work-group's keys; below, a
+// fixed step of 2^-34 of it. A smaller slack reaches further and raises more often:
+// grouped layer over 32k in MXFP4, multi-query one over 16k in fp8 and grouped
+// differential one over 16k in MXFP4 in turn 180, 58 and 37.3 us with 8, 180.5, 58 and
+// 37.4 with 5, 182, 60 and 38.0 with 4, 193, 66 and 43.6 with 2. E4M3 values are exact
+// in fp16. MXFP4 values enter relative to the largest scale of the same 32 elements
+// among the work-group's keys, read ahead (1/16 of the chunk's value bytes), which
+// enters as 2^13 (the largest value is then 6 * 2^13 of fp16's 65504), and are exact
+// down to 2^-36 of it.
 template <int D, int NW, int SK, typename KV, int MAPS>
 __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigned char* lds) {
   constexpr int KD = D / MAPS;             // dims of the logits
@@ -929,10 +929,10 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
           if (8 * (v / 4) + 4 * h + (v & 3) >= nv) x[v] = kNegInf;
       }
       // Weights against the current reference first; a raise needs a weight
-      // above 2^kSlack (times 2^kUp), which shows in their sum.
+      // above 2^(kUp + kSlack), which shows in their sum.
       float pr[16], ps;
       auto weights = [&]() {
-        const float nbase = mref == kNegInf ? 0.f : kUp - mref;
+        const float nbase = mref == kNegInf ? 0.f : -mref;
 #pragma unroll
         for (int v = 0; v < 16; ++v) pr[v] = exp2_fast(__builtin_fmaf(x[v], sl2, nbase));
         ps = pr[0];
@@ -944,14 +944,18 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
         float lmax = x[0];
 #pragma unroll
         for (int v = 1; v < 16; ++v) lmax = fmaxf(lmax, x[v]);
-        const float tmax = xor32_max(lmax) * sl2;
-        const bool raise = tmax > mref + kSlack;
+        // by how much the largest logit exceeds the reference, in one rounding as
+        // in the weights: those of huge logits stay in fp16's range too
+        lmax = xor32_max(lmax);
+        const float tmax = lmax * sl2;
+        const bool raise = __builtin_fmaf(lmax, sl2, -mref) > kUp + kSlack;
         if (__any(raise)) {
-          const float alpha = raise ? exp2_fast(mref - tmax) : 1.f;
+          const float ref = tmax - kUp;  // whatever its rounding, the partial's own
+          const float alpha = raise ? exp2_fast(mref - ref) : 1.f;
           lsum *= alpha;
 #pragma unroll
           for (int t = 0; t < DB; ++t) acc[t] *= alpha;
-          mref = raise ? tmax : mref;
+          mref = raise ? ref : mref;
           weights();
         }
       }
@@ -989,8 +993,7 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
   }
   if (__any(bad) && lane == 0) atomicOr(P.status, kStatusPage);
   if (!active) return;
-  const float down = kHalf ? 0x1p-10f : 1.f;  // 2^-kUp
-  const float ltot = xor32_sum(lsum) * down;
+  const float ltot = xor32_sum(lsum);
   const int row = row0 + j;
   if (row < Mh) {
     const size_t prow = ((size_t)gam * P.S_c + s) * P.M + (size_t)map * Mh + row;
@@ -999,10 +1002,7 @@ __device__ __forceinline__ void ctx_many_block(const PagedAttnParams& P, unsigne
 #pragma unroll
       for (int t = 0; t < DB; ++t)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vrefs[t] - (int)kUp);
-    } else if constexpr (kHalf) {
-#pragma unroll
-      for (int t = 0; t < DB; ++t) acc[t] *= down;
+        for (int v = 0; v < 16; ++v) acc[t][v] = ldexpf(acc[t][v], vrefs[t]);
     }
 #pragma unroll
     for (int t = 0; t < DB; ++t)

@@ -298,3 +298,33 @@ def test_infinite_keys_of_one_map(case, map_, launches, monkeypatch):
     ref, tol = bounds(x, lam)
     assert torch.isfinite(got[-math.inf]).all()
     assert ((got[-math.inf] - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.93, 0.87, 0.79, 0.71])
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3", "mxfp4"])
+@pytest.mark.parametrize("case", MANY[:2], ids=IDS[:2])
+def test_differences_of_huge_logits(case, kv, scale):
+    """Logits 2^25 and 2^25 + 4, whose differences are exact: the weights are those
+    of 0 and 4."""
+    *dims, _ = case
+    x = Problem(*dims, kv, seed=71, scaled=False)
+    x.q[:] = 0
+    x.q[..., 0], x.q[..., 1] = 2.0 ** 25, 1
+    K = {name: torch.zeros_like(getattr(x, name)["K"]) for name in ("ctx", "own")}
+    for rows in K.values():
+        rows[..., 0] = 1
+    K["ctx"][:, 300:, 1] = 4
+    put(x, K)
+    got = attend(x, scale=scale)
+    pos = torch.arange(x.m_c + x.m_d)
+    own = (x.lens.view(-1, 1) - x.n + 1 + torch.arange(x.n)).clamp(min=0)  # [b, n]
+    seen = pos < x.m_c + own.unsqueeze(-1)
+    e = torch.where(seen, torch.where((pos >= 300) & (pos < x.m_c), 1.0, math.exp(-4 * scale)), 0.0).double()[:, None]
+    V = torch.cat((x.ctx["V"].expand(x.b, *x.ctx["V"].shape), x.own["V"]), 2)
+    V = torch.where((pos < x.m_c + x.lens.view(-1, 1))[:, None, :, None], V, 0.0)
+    e = e / e.sum(-1, keepdim=True)
+    ref, size = ((e @ v).repeat_interleave(x.h // x.g, 1) for v in (V, V.abs()))
+    # the scale's own rounding, 2^-24 of the difference; the sums' order
+    tol = HALF_BF16 * ref.abs() + (1 + HALF_BF16) * (2.0 ** -11 + EPS32 * (8 + 2 * pos.numel())) * size
+    print("largest error", ((got - ref).abs() / tol).max().item(), "of the tolerance", flush=True)
+    assert ((got - ref).abs() <= tol).all()
