@@ -260,14 +260,15 @@ template <int D> __device__ __forceinline__ bool has_odd_values(const unsigned c
   return __any((odd & 0x80008000u) != 0);
 }
 
-// Keys of the tile from `first` on that hold such values, and that later tokens
-// alone see: their weight in the rows before is 0, which the products would
-// turn into NaN. They enter the rows that see them one by one and leave the tile.
+// Keys of the tile that hold such values and that later tokens alone see (row r
+// sees those below all + r % ntok): their weight in the rows before is 0, which the
+// products would turn into NaN. They enter the rows that see them one by one,
+// whatever the weight, and leave the tile.
 template <int D, int NT>
 __device__ __forceinline__ void take_odd_values(PageState<D, NT>& st, unsigned char* vl, const u32x4* hi, const u32x4* lo,
-                                             int first, int lane) {
+                                             int all, int ntok, int lane) {
 #pragma unroll 1
-  for (int key = first; key < kTileKeys; ++key) {
+  for (int key = max(0, all); key < kTileKeys; ++key) {
     unsigned char* row = vl + key * PageRow<D>::VROW;
     const u32x4 own = *(volatile const lds_u32x4*)(row + 16 * (lane % (D / 8)));
     bool odd = false;
@@ -283,7 +284,7 @@ __device__ __forceinline__ void take_odd_values(PageState<D, NT>& st, unsigned c
         if (w == e / 2) a = hi[nt][w], b = lo[nt][w];
       const int up = e % 2 ? 0 : 16;
       const float p = __shfl(__uint_as_float(a << up & 0xffff0000u) + __uint_as_float(b << up & 0xffff0000u), from);
-      if (!(p == 0.f))
+      if (key < all + (nt * kRowsPerTile + (lane & 15)) % ntok)
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) {
           const u32x2 v = *(volatile const lds_u32x2*)(row + 32 * t + 8 * (lane >> 4));
@@ -398,7 +399,7 @@ __device__ __forceinline__ void page_update(PageState<D, NT>& st, const PageTile
     lo[nt] = u32x4{o[0], o[1], o[2], o[3]};
   }
   if (ntok > 1 && rem < kTileKeys + ntok - 1 && has_odd_values<D>(vl, lane))
-    take_odd_values<D, NT>(st, vl, hi, lo, max(0, rem - (ntok - 1)), lane);
+    take_odd_values<D, NT>(st, vl, hi, lo, rem - (ntok - 1), ntok, lane);
 #pragma unroll
   for (int t = 0; t < DV; ++t) {
     const u32x4 v = PageTile<D, KV>::vop(vl, t, lane);

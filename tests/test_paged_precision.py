@@ -328,3 +328,27 @@ def test_differences_of_huge_logits(case, kv, scale):
     tol = HALF_BF16 * ref.abs() + (1 + HALF_BF16) * (2.0 ** -11 + EPS32 * (8 + 2 * pos.numel())) * size
     print("largest error", ((got - ref).abs() / tol).max().item(), "of the tolerance", flush=True)
     assert ((got - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("launches", ["parts", "one launch"])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_nonfinite_values_without_weight(value, launches, monkeypatch):
+    """A draft token's row with an infinity or a NaN in its value and a key that
+    leaves it no weight makes NaN of the tokens that see it, as 0 times it is, and
+    of no other."""
+    monkeypatch.setenv("BIFATTN_WHOLE", "2" if launches == "parts" else "1")
+    lens = [70, 33, 64, 40]
+    x = Problem(4, 6, 2, 128, 20, 70, n=4, page=16, kv="bf16", lens=lens, seed=13)
+    x.q[..., 3] = 1
+    K, V = ({name: getattr(x, name)[k].clone() for name in ("ctx", "own")} for k in "KV")
+    for i, length in enumerate(lens):
+        K["own"][i, 1, length - 3, 3] = -2.0 ** 40  # the second token's row
+    put(x, K)
+    want = attend(x)
+    for i, length in enumerate(lens):
+        V["own"][i, 1, length - 3, 5] = value
+    put(x, V=V)
+    got = attend(x)
+    seen = torch.zeros_like(got, dtype=torch.bool)
+    seen[:, 3:, 1:, 5] = True
+    assert torch.isnan(got[seen]).all() and torch.equal(got[~seen], want[~seen])
