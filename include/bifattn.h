@@ -484,7 +484,8 @@ bifattn_status_t bifattn_paged_decode(bifattn_paged_plan_t plan, const void *q,
  *   out = out_scale * y,  or with weight (fp32 [d]):
  *   out = out_scale * weight * y / sqrt(mean(y^2) + eps)
  * (0 where y is 0 throughout, whatever eps). lambda: fp32 [h]; eps >= 0; the
- * norm is formed in 32 bits, at any size of y. Everything else as in bifattn_paged_decode.
+ * norm is formed in 32 bits, at any size of y. weight lies at a multiple of 16
+ * bytes (EALIGN), lambda of 4. Everything else as in bifattn_paged_decode.
  */
 bifattn_status_t bifattn_paged_decode_diff(bifattn_paged_plan_t plan, const void *q,
                                            const bifattn_pages_t *pages, const int32_t *ctx_table,

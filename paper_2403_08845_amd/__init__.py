@@ -731,7 +731,7 @@ def bifattn_paged_decode(plan: PagedPlan, q, pages: Pages, ctx_table, tables, le
 def bifattn_paged_decode_diff(plan: PagedPlan, q, pages: Pages, ctx_table, tables, lens, lam, out, *,
                               weight=None, eps=1e-5, out_scale=1.0, stream=None):
     """Enqueue one step of differential attention (plans with maps = 2): lam
-    fp32 [h], weight fp32 [d] or None (heads are not normalised)."""
+    fp32 [h], weight fp32 [d], 16-byte aligned, or None (heads are not normalised)."""
     caller = getattr(plan, "_caller", None)
     if caller is not None and _taken(caller.diff(q, pages, ctx_table, tables, lens, out, lam, weight, eps, out_scale,
                                           None if stream is None else _stream_ptr(stream).value or 0), "bifattn_paged_decode_diff"):

@@ -62,3 +62,25 @@ def test_one_context_table_for_all_calls(native):
         with pytest.raises(ValueError):
             bif.bifattn_paged_gather(plan, pages, table[:, :-1], length, *outs, context=True)
         plan._caller = caller
+
+
+def test_alignment_of_the_norm_weight():
+    """A weight in the middle of a fused buffer is refused unless it lies at a
+    multiple of 16 bytes; the output is left as it was."""
+    x = Problem(2, 4, 2, 64, 20, 12, page=16, maps=2, lens=[12, 5], seed=2)
+    fused = torch.randn(64 * 3, generator=x.rng).cuda()
+    lam = fused[1:5]  # 4 bytes are enough
+    args = (x.q.cuda(), x.pages(), x.ctx_table.cuda(), x.tables.cuda(), x.lens.cuda(), lam)
+    out = torch.full((2, 4, 1, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    with x.plan() as plan:
+        for at in (1, 2, 3, 66):
+            with pytest.raises(bif.BifattnError) as e:
+                bif.bifattn_paged_decode_diff(plan, *args, out, weight=fused[at:at + 64])
+            assert e.value.status == bif.EALIGN
+        torch.cuda.synchronize()
+        assert (out == 3.0).all()
+        other = torch.zeros_like(out)
+        bif.bifattn_paged_decode_diff(plan, *args, out, weight=fused[68:132])
+        bif.bifattn_paged_decode_diff(plan, *args, other, weight=fused[68:132].clone())
+        assert bif.bifattn_paged_plan_status(plan) == bif.OK
+        assert torch.equal(out, other) and bool(out.isfinite().all())
