@@ -50,22 +50,26 @@ __device__ __forceinline__ void rotate(float& x, float& y, const Turn& a) {
   y = __builtin_fmaf(x, a[2], y * a[0]) + finite_rest(__builtin_fmaf(x, a[3], y * a[1]));
   x = p;
 }
-// The same in 64 bits, scaled and rounded to odd, for codes: an element next
+// The same in 64 bits, then rounded to odd, for codes: an element next
 // to a border between two codes falls on its side, where it is 2^-50 of |x| + |y| or
 // more away from it.
-template <typename S> __device__ __forceinline__ void rotate_odd(float& x, float& y, const FullTurn& a, const S& scaled) {
+template <typename R> __device__ __forceinline__ void rotate_odd(float& x, float& y, const FullTurn& a, const R& rounded) {
   const double u = x, v = y;
-  x = odd_f32(scaled(u * a[0] - v * a[1]));
-  y = odd_f32(scaled(u * a[1] + v * a[0]));
+  x = rounded(u * a[0] - v * a[1]);
+  y = rounded(u * a[1] + v * a[0]);
 }
-// x / scale, correctly rounded: the product with the rounded reciprocal alone may
-// miss a quotient in the middle between two codes (147 / 49 is 3). Infinities and
-// quotients past the codes' range keep the product.
-struct OverScale {
+// x / scale, rounded to odd: the fp32 value f near x times the rounded reciprocal
+// is compared with the quotient itself by f * scale (48 bits, exact), which that
+// product misses where it is short (147 / 49 is 3). Past fp32's range the largest
+// value, which saturates as a code; NaN stays.
+struct OddQuotient {
   double scale, inv;
-  __device__ __forceinline__ double operator()(double x) const {
-    const double q = x * inv;
-    return fabs(q) < 1e6 ? __builtin_fma(__builtin_fma(-q, scale, x), inv, q) : q;
+  __device__ __forceinline__ float operator()(double x) const {
+    const float f = (float)(x * inv);
+    const double back = (double)f * scale;
+    if (back == x) return f;
+    const uint32_t u = __float_as_uint(f) - (fabs(back) > fabs(x) ? 1u : 0u);
+    return __uint_as_float(u | 1u);
   }
 };
 // Two chunks of 8 whose elements rotate with `turn`: with each other, or in
@@ -236,20 +240,20 @@ __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(
       const float* sc = is_k ? A.pool.k_scale : A.pool.v_scale;
       const float s = sc ? sc[gam] : 1.f;
       if (t == 0 && !(s >= __FLT_MIN__ && s <= __FLT_MAX__)) atomicOr(A.status, kStatusScale);
-      const OverScale over = {(double)s, 1.0 / (double)s};
+      const OddQuotient over = {(double)s, 1.0 / (double)s};
       if (rotates) {
         rotate_chunks(fx, fy, full + first, A.neighbours,
                       [&](float& x, float& y, const FullTurn& a) { rotate_odd(x, y, a, over); });
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) fx[e] = odd_f32(over(fx[e])), fy[e] = odd_f32(over(fy[e]));
+        for (int e = 0; e < 8; ++e) fx[e] = over(fx[e]), fy[e] = over(fy[e]);
       }
       *reinterpret_cast<u32x2*>(dst + 8 * c0) = to_fp8(fx);
       *reinterpret_cast<u32x2*>(dst + 8 * c1) = to_fp8(fy);
     } else {
       if (rotates)
         rotate_chunks(fx, fy, full + first, A.neighbours,
-                      [&](float& x, float& y, const FullTurn& a) { rotate_odd(x, y, a, [](double v) { return v; }); });
+                      [&](float& x, float& y, const FullTurn& a) { rotate_odd(x, y, a, odd_f32); });
       // A block is four chunks, of several of the row's threads: their
       // exponents meet in LDS. A row's threads are neighbours in one wave,
       // whose LDS accesses execute in order.
