@@ -661,7 +661,7 @@ __device__ __forceinline__ void ctx_few_block(const PagedAttnParams& P, int blk,
 // Grid: n_ctx_small_blocks context work-groups, then n_dec_blocks decode ones.
 // Over bf16 bound by memory: 32 samples of a 32-head layer over 8k rows 66 us
 // for 403 MB, 6.1 TB/s. Over MXFP4 (107 MB, 29 us) by the work and the latency of
-// a tile: vector units 42%, matrix cores 20% of the cycles, a third of the waves'
+// a tile: vector units 48%, matrix cores 22% of the cycles, a third of the waves'
 // time waiting for memory; registers for three waves per SIMD instead of two hide
 // more of it (31.5, so 29). More query tiles need the registers of two, or one.
 template <int D, typename KV, int NTC, int NTD>
@@ -703,9 +703,10 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(PagedAttnParams P) {
 // stage. With maps = 2 a row block belongs to one map, whose half of the key
 // rows alone enters its logits.
 //
-// Bound by what a block of 32 keys costs a CU: matrix cores, vector units and
-// LDS are each busy for about half of the cycles (256 samples of a grouped layer
-// over 32k rows in MXFP4: 176 us a step, 790 TFLOP/s).
+// Bound by what a block of 32 keys costs a CU: matrix cores, vector units and LDS
+// take turns, each busy for 40 to 47% of the cycles of the CUs that have work (256
+// samples of a grouped layer over 32k rows in MXFP4: 178 us a step, 790 TFLOP/s),
+// and by the CUs of the own rows, which end early.
 //
 // Code caches take fp16 for the value product: one term of 11 bits for the weights
 // (their error 2e-4 beside the output's 1.7e-3) where bf16 values need two. The
